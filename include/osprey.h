@@ -409,6 +409,122 @@ int osprey_graph_capture(osprey_handle* h, const osprey_step_args* step, int32_t
 int osprey_graph_launch(osprey_handle* h, osprey_graph* g);
 int osprey_graph_destroy(osprey_graph* g);
 
+/* A paged key/value cache held in 8 bits, without a handle: for the attention of a target
+ * that is verified here, or any body that the caller runs.  (A drafter takes the same cache
+ * with dtype OSPREY_BF16_KV8.)  Half of a bf16 cache's bytes per position.
+ *
+ * Pages hold 16 positions.  Position t of sequence b is token t % 16 of physical page
+ * page_table[b][t / 16].  Page p has, per kv head, 16 head_dim key codes and as many value
+ * codes at codes + p * page_stride, as [2 (keys, values)][n_kv_heads][16 head_dim], and two
+ * scales at scales + p * scale_stride, as [n_kv_heads][2 (keys, values)].  Codes are e4m3
+ * (OCP: finite, magnitudes up to 448), scales powers of two, value = code * scale.  Within a
+ * block keys are [16][head_dim] and values [4][16][head_dim / 16][4]: token t, dim e at
+ * [t / 4][e % 16][e / 16][t % 4].  Strides let one pool hold the pages of several layers.
+ * A page belongs to one sequence.  Memory need not be cleared: no call reads a position that
+ * was not written, but what a caller writes there itself must be finite codes.
+ *
+ * Device conditions (err, nullable, a device word that the calls only set bits of): bit 2 a
+ * row sees positions without a page (skipped), bit 3 a write to a position without a page
+ * (skipped) or a kept path that does not ascend, bit 6 a key or value that is not finite
+ * (stored as zero), bit 7 a rotation position outside the table (clamped). */
+typedef struct {
+  const int32_t* page_table;  /* [batch][max_pages] */
+  int32_t batch;              /* sequences: 1 .. 4096 */
+  int32_t max_pages;          /* capacity of a sequence: 16 max_pages positions, under 2^31 */
+  int32_t num_pages;          /* physical pages */
+  int32_t n_kv_heads;
+  int32_t head_dim;           /* 64 or 128 */
+  void* codes;                /* 16-byte aligned */
+  int64_t page_stride;        /* bytes; a multiple of 16, at least 32 n_kv_heads head_dim */
+  float* scales;
+  int64_t scale_stride;       /* floats; at least 2 n_kv_heads */
+} osprey_kv8_cache;
+
+/* Arguments of osprey_kv8_append.  Sequence b has rows cu_rows[b] .. cu_rows[b + 1] - 1 of
+ * `rows` (cu_rows NULL: one row each, rows == batch), which take the positions cached[b],
+ * cached[b] + 1, ...  Rows behind cu_rows[batch] are neither read nor written.
+ * Queries and keys are normalised per head (x gain / sqrt(mean x^2 + eps), where the gain is
+ * given) and rotated by halves with the cosines and sines of the row's position (rope_pos, or
+ * the cache position where that is NULL; rope_cos NULL: no rotation); queries go to q_out,
+ * keys and values into the cache.  Per block (page, kv head, keys or values) the scale becomes
+ * the smallest power of two, at least 2^-100, that takes the new elements to at most 448; a
+ * block that holds older positions (the first new one is not the page's first) keeps at least
+ * its old scale, and where the scale grows the older codes are rounded to it.  Codes are
+ * rounded to nearest, ties to even, keys from double. */
+typedef struct {
+  int32_t rows;
+  const int32_t* cu_rows;     /* [batch + 1] or NULL */
+  const int32_t* cached;      /* [batch] positions before the new rows */
+  const int32_t* rope_pos;    /* [rows] or NULL */
+  int32_t dtype;              /* osprey_dtype of q, k, v, the gains and q_out */
+  int32_t n_q_heads;          /* ignored when q is NULL */
+  const void* q;              /* row r at q + r * q_stride (elements): [n_q_heads][head_dim]; or NULL */
+  const void* k;              /* likewise [n_kv_heads][head_dim] */
+  const void* v;
+  int64_t q_stride, k_stride, v_stride;   /* rows on 16-byte boundaries */
+  const void* q_norm;         /* [head_dim] or NULL */
+  const void* k_norm;
+  float eps;
+  const float* rope_cos;      /* [rope_len][head_dim / 2] or NULL (both) */
+  const float* rope_sin;
+  int32_t rope_len;
+  void* q_out;                /* row r at q_out + r * q_out_stride; not NULL with q; may be q */
+  int64_t q_out_stride;
+  uint32_t* err;              /* or NULL */
+} osprey_kv8_append_args;
+
+/* Arguments of osprey_kv8_attention: out_r = sum_t softmax_t(scale q_r . k_t) v_t over the
+ * positions that row r sees, the new rows' own positions already appended.  Row j of sequence
+ * b sees the positions up to and including cached[b] + j; with a tree mask the positions
+ * before cached[b], and cached[b] + i where bit i % 64 of tree_mask[2 r + i / 64] is set (at
+ * most 128 rows a sequence).  A row that sees nothing gets zeros.  Sums are held in fp32.
+ * Query head h reads kv head h n_kv_heads / n_q_heads.
+ * max_rows (at least the largest row count of a sequence) and max_context (the longest context
+ * with its new rows that the call is planned for) only choose the kernel and how the work is
+ * split: longer sequences are still attended right.  The work is dealt out on the device from
+ * the lengths there, so that a captured call serves every later length.
+ * The workspace holds the splits' partial outputs and nothing that outlives a call: calls in
+ * order on one stream may share one, calls that can overlap may not. */
+typedef struct {
+  int32_t rows;
+  int32_t max_rows;
+  int32_t max_context;
+  const int32_t* cu_rows;     /* [batch + 1] or NULL */
+  const int32_t* cached;      /* [batch] */
+  const uint64_t* tree_mask;  /* [rows][2] or NULL */
+  int32_t dtype;              /* osprey_dtype of q and out */
+  int32_t n_q_heads;          /* a multiple of n_kv_heads */
+  const void* q;              /* row r at q + r * q_stride (elements): [n_q_heads][head_dim] */
+  int64_t q_stride;
+  float scale;                /* > 0 (usually 1 / sqrt(head_dim)) */
+  void* out;                  /* row r at out + r * out_stride */
+  int64_t out_stride;
+  void* workspace;            /* 16-byte aligned */
+  size_t workspace_bytes;
+  uint32_t* err;              /* or NULL */
+} osprey_kv8_attention_args;
+
+/* Arguments of osprey_kv8_keep: position base[b] + i takes the keys and values of position
+ * base[b] + path[b][i], i < n[b], by the append's rule for scales (a row of osprey_verify_tree's
+ * accept_path with base = the position of node 0, and n = accept_len).  A path ascends. */
+typedef struct {
+  const int32_t* base;        /* [batch] */
+  const int32_t* path;        /* [batch][path_stride] */
+  int32_t path_stride;
+  const int32_t* n;           /* [batch]; at most path_stride is taken */
+  uint32_t* err;              /* or NULL */
+} osprey_kv8_keep_args;
+
+/* The calls are enqueued on hip_stream (NULL: the null stream) of the current device, which
+ * must be the buffers'; they allocate nothing, keep nothing, and can be captured into a graph.
+ * osprey_kv8_workspace_bytes: the workspace of an attention call with these sizes (0: invalid,
+ * or no device). */
+int osprey_kv8_append(const osprey_kv8_cache* c, const osprey_kv8_append_args* a, void* hip_stream);
+size_t osprey_kv8_workspace_bytes(const osprey_kv8_cache* c, int32_t rows, int32_t n_q_heads, int32_t max_rows,
+                                  int32_t max_context);
+int osprey_kv8_attention(const osprey_kv8_cache* c, const osprey_kv8_attention_args* a, void* hip_stream);
+int osprey_kv8_keep(const osprey_kv8_cache* c, const osprey_kv8_keep_args* a, void* hip_stream);
+
 /* Synchronise, read and clear the device error flags (host out):
  * bit 0 an ingest row count outside [1, max new rows] (pending without verify),
  * bit 1 a token id outside [0, V_T), bit 2 a sequence beyond its KV pages,

@@ -74,6 +74,37 @@ class osprey_tree_args(C.Structure):
                 ("tokens", C.c_void_p), ("parents", C.c_void_p), ("scores", C.c_void_p)]
 
 
+class osprey_kv8_cache(C.Structure):
+    _fields_ = [("page_table", C.c_void_p), ("batch", C.c_int32), ("max_pages", C.c_int32),
+                ("num_pages", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("codes", C.c_void_p), ("page_stride", C.c_int64), ("scales", C.c_void_p),
+                ("scale_stride", C.c_int64)]
+
+
+class osprey_kv8_append_args(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("cu_rows", C.c_void_p), ("cached", C.c_void_p),
+                ("rope_pos", C.c_void_p), ("dtype", C.c_int32), ("n_q_heads", C.c_int32),
+                ("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("q_stride", C.c_int64),
+                ("k_stride", C.c_int64), ("v_stride", C.c_int64), ("q_norm", C.c_void_p),
+                ("k_norm", C.c_void_p), ("eps", C.c_float), ("rope_cos", C.c_void_p),
+                ("rope_sin", C.c_void_p), ("rope_len", C.c_int32), ("q_out", C.c_void_p),
+                ("q_out_stride", C.c_int64), ("err", C.c_void_p)]
+
+
+class osprey_kv8_attention_args(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("max_rows", C.c_int32), ("max_context", C.c_int32),
+                ("cu_rows", C.c_void_p), ("cached", C.c_void_p), ("tree_mask", C.c_void_p),
+                ("dtype", C.c_int32), ("n_q_heads", C.c_int32), ("q", C.c_void_p),
+                ("q_stride", C.c_int64), ("scale", C.c_float), ("out", C.c_void_p),
+                ("out_stride", C.c_int64), ("workspace", C.c_void_p),
+                ("workspace_bytes", C.c_size_t), ("err", C.c_void_p)]
+
+
+class osprey_kv8_keep_args(C.Structure):
+    _fields_ = [("base", C.c_void_p), ("path", C.c_void_p), ("path_stride", C.c_int32),
+                ("n", C.c_void_p), ("err", C.c_void_p)]
+
+
 _P = C.c_void_p
 _H = C.c_void_p
 SIGNATURES = {
@@ -104,6 +135,12 @@ SIGNATURES = {
     "osprey_graph_launch": (C.c_int, [_H, _P]),
     "osprey_graph_destroy": (C.c_int, [_P]),
     "osprey_draft_destroy": (C.c_int, [_H]),
+    "osprey_kv8_append": (C.c_int, [C.POINTER(osprey_kv8_cache), C.POINTER(osprey_kv8_append_args), _P]),
+    "osprey_kv8_workspace_bytes": (C.c_size_t, [C.POINTER(osprey_kv8_cache), C.c_int32, C.c_int32,
+                                                C.c_int32, C.c_int32]),
+    "osprey_kv8_attention": (C.c_int, [C.POINTER(osprey_kv8_cache),
+                                       C.POINTER(osprey_kv8_attention_args), _P]),
+    "osprey_kv8_keep": (C.c_int, [C.POINTER(osprey_kv8_cache), C.POINTER(osprey_kv8_keep_args), _P]),
     "osprey_last_error": (C.c_char_p, []),
 }
 

@@ -401,6 +401,172 @@ def verify_rows_static(K: int, target_logits, draft_logits, draft_tokens, temper
                                             C.c_void_p(st.cuda_stream)))
 
 
+# -- the 8-bit cache (osprey_kv8_*) --------------------------------------------------------
+
+class Kv8Cache:
+    """A paged key/value cache held in 8 bits (osprey_kv8_cache): codes uint8 [pages, 2,
+    n_kv_heads, 16 * head_dim], scales float32 [pages, n_kv_heads, 2], page_table int32
+    [batch, max_pages].  codes and scales may be strided over the pages (one layer of a pool);
+    memory need not be cleared."""
+
+    def __init__(self, codes, scales, page_table, head_dim: int):
+        import torch
+        if codes.dim() != 4 or codes.dtype != torch.uint8 or codes.shape[1] != 2 or codes.shape[3] != 16 * head_dim:
+            raise ValueError(f"codes: need uint8 [pages, 2, n_kv_heads, {16 * head_dim}], got {codes.dtype} {tuple(codes.shape)}")
+        pages, _, nkv, w = codes.shape
+        if scales.dtype != torch.float32 or tuple(scales.shape) != (pages, nkv, 2):
+            raise ValueError(f"scales: need float32 {(pages, nkv, 2)}, got {scales.dtype} {tuple(scales.shape)}")
+        if page_table.dtype != torch.int32 or page_table.dim() != 2 or not page_table.is_contiguous():
+            raise ValueError("page_table: need a contiguous int32 [batch, max_pages]")
+        if codes.stride()[1:] != (nkv * w, w, 1) or scales.stride()[1:] != (2, 1):
+            raise ValueError("codes and scales: a page must be contiguous")
+        self.device = _same_device(codes, scales, page_table)
+        self.codes, self.scales, self.page_table = codes, scales, page_table   # kept: the struct holds raw pointers
+        self.batch, self.n_kv_heads, self.head_dim = int(page_table.shape[0]), nkv, head_dim
+        # (one page: its stride is not used, and torch gives any)
+        self.c = L.osprey_kv8_cache(_ptr(page_table), self.batch, int(page_table.shape[1]), pages, nkv, head_dim,
+                                    _ptr(codes), codes.stride(0) if pages > 1 else 2 * nkv * w, _ptr(scales),
+                                    scales.stride(0) if pages > 1 else 2 * nkv)
+
+
+def _same_device(*tensors):
+    dev = tensors[0].device
+    for t in tensors:
+        if t is not None and (t.device != dev or not t.is_cuda):
+            raise ValueError(f"need tensors of one GPU, got {dev} and {t.device}")
+    return dev
+
+
+def _ints(t, numel: int, name: str):
+    import torch
+    if t is not None and (t.dtype != torch.int32 or not t.is_contiguous() or t.numel() < numel):
+        raise ValueError(f"{name}: need {numel} contiguous int32, got {t.dtype} {tuple(t.shape)}")
+    return t
+
+
+def _heads(t, rows: int, hd: int, dtype, name: str) -> int:
+    """The row stride of [rows, heads, hd] whose heads are contiguous."""
+    if t.dim() != 3 or t.dtype != dtype or t.shape[0] != rows or t.shape[2] != hd:
+        raise ValueError(f"{name}: need {dtype} [{rows}, heads, {hd}], got {t.dtype} {tuple(t.shape)}")
+    if t.stride(2) != 1 or (t.stride(1) != hd and t.shape[1] > 1):
+        raise ValueError(f"{name}: the heads of a row must be contiguous")
+    return t.stride(0) if rows > 1 else t.shape[1] * hd
+
+
+def _kv8_dtype(t) -> int:
+    import torch
+    if t.dtype == torch.bfloat16:
+        return L.OSPREY_BF16
+    if t.dtype == torch.float32:
+        return L.OSPREY_F32
+    raise ValueError(f"dtype {t.dtype}: need bfloat16 or float32")
+
+
+class _on:
+    """The device of a call's buffers as the current one, and the stream to enqueue on."""
+
+    def __init__(self, device, stream):
+        import torch
+        self.guard = torch.cuda.device(device) if device.index != torch.cuda.current_device() else None
+        self.stream = stream if stream is not None else torch.cuda.current_stream(device)
+
+    def __enter__(self):
+        if self.guard:
+            self.guard.__enter__()
+        return C.c_void_p(self.stream.cuda_stream)
+
+    def __exit__(self, *e):
+        if self.guard:
+            self.guard.__exit__(*e)
+
+
+def kv8_append(cache: Kv8Cache, k, v, cached, q=None, q_out=None, cu_rows=None, rope_pos=None, q_norm=None, k_norm=None,
+               eps: float = 1e-6, rope_cos=None, rope_sin=None, errors=None, stream=None) -> None:
+    """osprey_kv8_append: k, v [rows, n_kv_heads, head_dim] (rows may be strided: a slice of a
+    QKV product) into the cache at positions cached[b] + j, and q [rows, n_q_heads, head_dim]
+    into q_out, normalised per head where a gain is given and rotated where rope_cos / rope_sin
+    [positions, head_dim / 2] are.  cu_rows int32 [batch + 1] groups the rows (None: one row
+    per sequence).  errors: an int32 device word whose bits the kernels set."""
+    import torch
+    rows, hd, dt = int(k.shape[0]), cache.head_dim, k.dtype
+    a = L.osprey_kv8_append_args()
+    a.dtype = _kv8_dtype(k)
+    _same_device(cache.codes, k, v, cached, q, q_out, cu_rows, rope_pos, q_norm, k_norm, rope_cos, rope_sin, errors)
+    a.rows = rows
+    a.k_stride, a.v_stride = _heads(k, rows, hd, dt, "k"), _heads(v, rows, hd, dt, "v")
+    if k.shape[1] != cache.n_kv_heads or v.shape[1] != cache.n_kv_heads:
+        raise ValueError(f"k and v: need {cache.n_kv_heads} heads")
+    a.k, a.v = _ptr(k), _ptr(v)
+    if q is not None:
+        if q_out is None or q_out.shape != q.shape:
+            raise ValueError("q_out: need a tensor of q's shape")
+        a.q, a.q_stride, a.q_out, a.q_out_stride = _ptr(q), _heads(q, rows, hd, dt, "q"), _ptr(q_out), _heads(q_out, rows, hd, dt, "q_out")
+        a.n_q_heads = int(q.shape[1])
+    for t, name in ((q_norm, "q_norm"), (k_norm, "k_norm")):
+        if t is not None and (t.dtype != dt or t.numel() != hd or not t.is_contiguous()):
+            raise ValueError(f"{name}: need {hd} contiguous {dt}")
+    a.q_norm, a.k_norm, a.eps = _ptr(q_norm), _ptr(k_norm), eps
+    if rope_cos is not None:
+        for t in (rope_cos, rope_sin):
+            if t is None or t.dtype != torch.float32 or t.dim() != 2 or t.shape[1] != hd // 2 or not t.is_contiguous() \
+                    or t.shape != rope_cos.shape:
+                raise ValueError(f"rope_cos and rope_sin: need contiguous float32 [positions, {hd // 2}] of one shape")
+        a.rope_cos, a.rope_sin, a.rope_len = _ptr(rope_cos), _ptr(rope_sin), int(rope_cos.shape[0])
+    a.cu_rows, a.cached = _ptr(_ints(cu_rows, cache.batch + 1, "cu_rows")), _ptr(_ints(cached, cache.batch, "cached"))
+    a.rope_pos, a.err = _ptr(_ints(rope_pos, rows, "rope_pos")), _ptr(_ints(errors, 1, "errors"))
+    with _on(cache.device, stream) as st:
+        _check(_lib().osprey_kv8_append(C.byref(cache.c), C.byref(a), st))
+
+
+def kv8_attention_workspace(cache: Kv8Cache, rows: int, n_q_heads: int, max_rows: int, max_context: int) -> int:
+    """Bytes of the workspace of a kv8_attention call with these sizes."""
+    with _on(cache.device, None):
+        n = int(_lib().osprey_kv8_workspace_bytes(C.byref(cache.c), rows, n_q_heads, max_rows, max_context))
+    if n == 0:
+        raise OspreyError(L.OSPREY_E_INVALID, last_error())
+    return n
+
+
+def kv8_attention(cache: Kv8Cache, q, out, cached, workspace, max_rows: int = 1, max_context: int = 1, cu_rows=None,
+                  scale=None, tree_mask=None, errors=None, stream=None) -> None:
+    """osprey_kv8_attention: out [rows, n_q_heads, head_dim] = attention of q over what the rows
+    see of the cache (their own positions already appended).  tree_mask int64 [rows, 2]: the
+    bits of the new positions that a row sees.  max_rows, max_context: the largest row count and
+    context the call is planned for.  workspace: uint8, kv8_attention_workspace bytes."""
+    import torch
+    rows, hd, dt = int(q.shape[0]), cache.head_dim, q.dtype
+    a = L.osprey_kv8_attention_args()
+    a.dtype = _kv8_dtype(q)
+    _same_device(cache.codes, q, out, cached, workspace, cu_rows, tree_mask, errors)
+    a.rows, a.max_rows, a.max_context = rows, int(max_rows), int(max_context)
+    if out.shape != q.shape:
+        raise ValueError("out: need a tensor of q's shape")
+    a.q, a.q_stride, a.out, a.out_stride = _ptr(q), _heads(q, rows, hd, dt, "q"), _ptr(out), _heads(out, rows, hd, dt, "out")
+    a.n_q_heads = int(q.shape[1])
+    a.scale = hd ** -0.5 if scale is None else scale
+    if tree_mask is not None and (tree_mask.dtype != torch.int64 or tuple(tree_mask.shape) != (rows, 2) or not tree_mask.is_contiguous()):
+        raise ValueError(f"tree_mask: need a contiguous int64 [{rows}, 2]")
+    a.tree_mask = _ptr(tree_mask)
+    if workspace.dtype != torch.uint8 or not workspace.is_contiguous():
+        raise ValueError("workspace: need a contiguous uint8 tensor")
+    a.workspace, a.workspace_bytes = _ptr(workspace), workspace.numel()
+    a.cu_rows, a.cached = _ptr(_ints(cu_rows, cache.batch + 1, "cu_rows")), _ptr(_ints(cached, cache.batch, "cached"))
+    a.err = _ptr(_ints(errors, 1, "errors"))
+    with _on(cache.device, stream) as st:
+        _check(_lib().osprey_kv8_attention(C.byref(cache.c), C.byref(a), st))
+
+
+def kv8_keep(cache: Kv8Cache, base, path, n, errors=None, stream=None) -> None:
+    """osprey_kv8_keep: position base[b] + i takes position base[b] + path[b, i], i < n[b]."""
+    _same_device(cache.codes, base, path, n, errors)
+    if path.dim() != 2 or path.shape[0] != cache.batch:
+        raise ValueError(f"path: need [{cache.batch}, nodes]")
+    a = L.osprey_kv8_keep_args(_ptr(_ints(base, cache.batch, "base")), _ptr(_ints(path, path.numel(), "path")), int(path.shape[1]),
+                               _ptr(_ints(n, cache.batch, "n")), _ptr(_ints(errors, 1, "errors")))
+    with _on(cache.device, stream) as st:
+        _check(_lib().osprey_kv8_keep(C.byref(cache.c), C.byref(a), st))
+
+
 class IterationGraph:
     """A captured iteration (osprey_graph_*): launch() enqueues it on the drafter's
     stream; close() releases it (after the stream has finished with it)."""

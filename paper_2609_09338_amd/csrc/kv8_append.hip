@@ -1,0 +1,515 @@
+// Writing the 8-bit cache (kv8.h): new rows' queries and keys are normalised per head and
+// rotated, and keys and values appended to the pages; the accepted path of a draft tree is
+// moved to the positions after its context.
+//
+//   x' = R(pos) (x * gain / sqrt(mean(x^2) + eps)),  R: (a, b) -> (a cos - b sin, b cos + a sin)
+//   scale of a block: the smallest 2^E >= amax / 448 over its new tokens, and not below the old
+//   one while it holds older tokens; code = rne8(x' / 2^E)
+//
+// Bound by memory: every projection is read once, every query and code written once.  The
+// scale of a block needs all of its new tokens, so a wavefront owns one block (page, kv head,
+// keys or values) and holds its 16 hd values in registers: one pass, no LDS, no atomics on
+// data, and the same codes whatever else is in the batch.
+// A code is a rounding to 4 bits: a key that is off by 2^-24 next to a border changes by a
+// sixteenth of itself.  Keys are therefore normalised and rotated in double (half of the fp32
+// rate here, and keys are the smaller part of a row), and rounded once: codes are those of the
+// definition, not of a summation order.  Values and queries need no more than fp32.
+#include "kv8.h"
+
+namespace osp {
+namespace {
+
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+template <typename T> OSP_DEV float gain_at(const void* g, int i) { return load_f32(reinterpret_cast<const T*>(g), i); }
+OSP_DEV float gain(const void* g, int bf16, int i) { return bf16 ? gain_at<bf16_t>(g, i) : gain_at<float>(g, i); }
+
+// N consecutive values of row r (N * sizeof(T) a multiple of 8), summed over K-split partials.
+template <typename T, int N>
+OSP_DEV void load_n(const void* base, long at, int ks, long split, float* x) {
+  const T* p = reinterpret_cast<const T*>(base) + at;
+  if constexpr (sizeof(T) == 2) {
+    if constexpr (N % 8 == 0) {
+#pragma unroll
+      for (int i = 0; i < N; i += 8) load_vec<bf16_t>(p + i, x + i);
+    } else {
+      static_assert(N == 2, "");
+      const uint32_t u = *reinterpret_cast<const uint32_t*>(p);
+      x[0] = bf16_lo(u);
+      x[1] = bf16_hi(u);
+    }
+  } else {
+    auto piece = [&](const float* s, float* y, bool add) {
+      if constexpr (N % 4 == 0) {
+#pragma unroll
+        for (int i = 0; i < N; i += 4) {
+          const float4 v = *reinterpret_cast<const float4*>(s + i);
+          y[i] = add ? y[i] + v.x : v.x;
+          y[i + 1] = add ? y[i + 1] + v.y : v.y;
+          y[i + 2] = add ? y[i + 2] + v.z : v.z;
+          y[i + 3] = add ? y[i + 3] + v.w : v.w;
+        }
+      } else {
+        static_assert(N == 2, "");
+        const float2 v = *reinterpret_cast<const float2*>(s);
+        y[0] = add ? y[0] + v.x : v.x;
+        y[1] = add ? y[1] + v.y : v.y;
+      }
+    };
+    piece(p, x, false);
+    for (int k = 1; k < ks; ++k) piece(p + k * split, x, true);
+  }
+}
+
+// x with its last bit set where the conversion dropped something: rounding the result again to
+// fewer bits equals rounding x once.
+OSP_DEV float to_float_odd(double x) {
+  const float f = (float)x;
+  int i = __float_as_int(f);
+  if ((double)f != x) {
+    if (fabs((double)f) > fabs(x)) --i;   // towards zero
+    i |= 1;
+  }
+  return __int_as_float(i);
+}
+
+// Smallest E in [kKv8MinExp, kKv8MaxExp] with amax <= 448 2^E.
+OSP_DEV int scale_exp(double amax) {
+  int e = kKv8MinExp;
+  if (amax > 0.0) {
+    const long long b = __double_as_longlong(amax);
+    // amax in [2^x, 2^(x + 1)); 448 = 1.75 2^8
+    const int x = (int)((b >> 52) & 2047) - 1023;
+    e = x - 8 + ((b & 0xfffffffffffffll) > 0xc000000000000ll ? 1 : 0);
+  }
+  return min(max(e, kKv8MinExp), kKv8MaxExp);
+}
+OSP_DEV int exp_of(float scale) { return min(max((int)((__float_as_uint(scale) >> 23) & 255) - 127, kKv8MinExp), kKv8MaxExp); }
+
+OSP_DEV uint32_t pack4(float a, float b, float c, float d) {
+  int u = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  u = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, u, true);
+  return (uint32_t)u;
+}
+OSP_DEV void unpack4(uint32_t u, float* x) {
+  const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)u, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)u, true);
+  x[0] = a[0];
+  x[1] = a[1];
+  x[2] = b[0];
+  x[3] = b[1];
+}
+OSP_DEV uint32_t shift4(uint32_t u, float f) {
+  float x[4];
+  unpack4(u, x);
+  return pack4(x[0] * f, x[1] * f, x[2] * f, x[3] * f);
+}
+
+OSP_DEV double wave_max_d(double v) {
+  v = fmax(v, dpp_d<kDppXor1>(v));
+  v = fmax(v, dpp_d<kDppXor2>(v));
+  v = fmax(v, dpp_d<kDppHalfMirror>(v));
+  v = fmax(v, dpp_d<kDppMirror>(v));
+  return fmax(fmax(lane_d(v, 0), lane_d(v, 16)), fmax(lane_d(v, 32), lane_d(v, 48)));
+}
+
+// A wavefront's lanes over a block.  Keys: token l / 4, dims NE (l % 4) .. + NE of either half.
+// Values: tokens 4 (l / 16) .. + 4, dims 16 d + 2 a and the one after, for the ND d's of its half.
+template <int HD> struct Lanes {
+  static constexpr int NE = HD / 8, ND = HD / 32;
+  int t, j;                // keys
+  int q, a, dh;            // values
+  OSP_DEV explicit Lanes(int lane) : t(lane >> 2), j(lane & 3), q(lane >> 4), a(lane & 7), dh((lane >> 3) & 1) {}
+  OSP_DEV int key_at(int half) const { return t * HD + half * (HD / 2) + j * NE; }
+  OSP_DEV int value_at(int odd) const { return q * 4 * HD + (2 * a + odd) * (HD / 4) + dh * ND * 4; }
+};
+
+// Key codes of lane's 2 NE values at 1 / scale; HD / 8 bytes per half.
+template <int HD>
+OSP_DEV void store_keys(uint8_t* blk, const Lanes<HD>& L, const float* x) {
+  constexpr int NE = HD / 8;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    uint32_t u[NE / 4];
+#pragma unroll
+    for (int i = 0; i < NE / 4; ++i) u[i] = pack4(x[h * NE + 4 * i], x[h * NE + 4 * i + 1], x[h * NE + 4 * i + 2], x[h * NE + 4 * i + 3]);
+    if constexpr (NE == 16) *reinterpret_cast<uint4*>(blk + L.key_at(h)) = make_uint4(u[0], u[1], u[2], u[3]);
+    else *reinterpret_cast<uint2*>(blk + L.key_at(h)) = make_uint2(u[0], u[1]);
+  }
+}
+
+// Older key codes (tokens before `off`) at a scale 1 / f times theirs.
+template <int HD>
+OSP_DEV void shift_keys(uint8_t* blk, const Lanes<HD>& L, int off, float f) {
+  if (L.t >= off) return;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    uint32_t* p = reinterpret_cast<uint32_t*>(blk + L.key_at(h));
+#pragma unroll
+    for (int i = 0; i < HD / 32; ++i) p[i] = shift4(p[i], f);
+  }
+}
+
+// Value codes of tokens [lo, hi) (x[i][odd][d], token 4 q + i) at 1 / scale; the older ones
+// (before lo) at f times their value.  Four tokens share a dword, so a partly new one is merged.
+template <int HD>
+OSP_DEV void store_values(uint8_t* blk, const Lanes<HD>& L, int lo, int hi, float f, bool shift, const float (*x)[2][HD / 32]) {
+  constexpr int ND = HD / 32;
+  const int t0 = 4 * L.q;
+  const int a = min(max(lo - t0, 0), 4), b = min(max(hi - t0, 0), 4);   // new tokens [a, b) of the four
+  if (a >= b && !(shift && a > 0)) return;
+  // bytes [a, b): new; [0, a): older; [b, 4): as they are
+  const uint32_t below_a = a >= 4 ? 0xffffffffu : (1u << 8 * a) - 1u;
+  const uint32_t below_b = b >= 4 ? 0xffffffffu : (1u << 8 * b) - 1u;
+  const uint32_t is_new = a < b ? below_b & ~below_a : 0u;
+#pragma unroll
+  for (int odd = 0; odd < 2; ++odd) {
+    uint32_t* p = reinterpret_cast<uint32_t*>(blk + L.value_at(odd));
+    uint32_t u[ND];
+#pragma unroll
+    for (int d = 0; d < ND; ++d) u[d] = pack4(x[0][odd][d], x[1][odd][d], x[2][odd][d], x[3][odd][d]);
+    if (is_new != 0xffffffffu) {
+#pragma unroll
+      for (int d = 0; d < ND; ++d) {
+        const uint32_t old = p[d];
+        const uint32_t older = shift ? (shift4(old, f) & below_a) | (old & ~below_a) : old;
+        u[d] = (u[d] & is_new) | (older & ~is_new);
+      }
+    }
+    if constexpr (ND == 4) *reinterpret_cast<uint4*>(p) = make_uint4(u[0], u[1], u[2], u[3]);
+    else *reinterpret_cast<uint2*>(p) = make_uint2(u[0], u[1]);
+  }
+}
+
+// The sequence of page unit u: sequence b's units begin at cu[b] / 16 + 2 b, which leaves room
+// for the pages that its rows touch (at most n / 16 + 2); with a row each, unit b is sequence b's.
+OSP_DEV int unit_seq(const Kv8Rows& r, int u) {
+  if (!r.cu) return u;
+  int lo = 0, hi = r.B - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) / 2;
+    if (r.cu[mid] / 16 + 2 * mid <= u) lo = mid;
+    else hi = mid - 1;
+  }
+  return lo;
+}
+
+template <typename T, int HD>
+OSP_DEV void append_keys(const Kv8AppendArgs& a, int b, const Kv8Seq& s, int r0, int off, int n, int g, uint8_t* blk,
+                         float* scale, int lane) {
+  constexpr int NE = HD / 8;
+  const Lanes<HD> L(lane);
+  const bool mine = L.t >= off && L.t < off + n;
+  const int row = r0 + L.t - off;
+  double x[2 * NE];
+  bool bad = false;
+  if (mine) {
+    float f[2 * NE];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      load_n<T, NE>(a.k, (long)row * a.ldk + (long)g * HD + h * (HD / 2) + L.j * NE, a.ks, a.split, f + h * NE);
+#pragma unroll
+    for (int i = 0; i < 2 * NE; ++i) x[i] = f[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < 2 * NE; ++i) x[i] = 0.0;
+  }
+  if (a.k_norm) {
+    double ss = 0.0;
+#pragma unroll
+    for (int i = 0; i < 2 * NE; ++i) ss += x[i] * x[i];
+    ss += dpp_d<kDppXor1>(ss);
+    ss += dpp_d<kDppXor2>(ss);
+    const double inv = 1.0 / sqrt(ss / HD + (double)a.eps);
+#pragma unroll
+    for (int i = 0; i < 2 * NE; ++i)
+      x[i] *= inv * (double)gain(a.k_norm, a.g_bf16, (i / NE) * (HD / 2) + L.j * NE + i % NE);
+  }
+  if (a.rope_cos && mine) {
+    const int p = a.rope_pos ? a.rope_pos[row] : s.first + row - s.beg;
+    if ((p < 0 || p >= a.max_pos) && a.err) atomicOr(a.err, 1u << 7);
+    const long c = (long)min(max(p, 0), a.max_pos - 1) * (HD / 2) + L.j * NE;
+#pragma unroll
+    for (int i = 0; i < NE; ++i) {
+      const double co = a.rope_cos[c + i], si = a.rope_sin[c + i], u = x[i], w = x[NE + i];
+      x[i] = u * co - w * si;
+      x[NE + i] = w * co + u * si;
+    }
+  }
+  double amax = 0.0;
+#pragma unroll
+  for (int i = 0; i < 2 * NE; ++i) {
+    if (!(fabs(x[i]) < 1.0e300)) {   // not finite (a finite input cannot come near this)
+      x[i] = 0.0;
+      bad = true;
+    }
+    amax = fmax(amax, fabs(x[i]));
+  }
+  if (bad && a.err) atomicOr(a.err, 1u << 6);
+  amax = wave_max_d(amax);
+  const int was = off > 0 ? exp_of(*scale) : kKv8MinExp;
+  const int e = max(scale_exp(amax), was);
+  if (off > 0 && e > was) shift_keys<HD>(blk, L, off, kv8_pow2(max(was - e, -126)));
+  if (mine) {
+    const double f = __longlong_as_double((long long)(1023 - e) << 52);
+    float y[2 * NE];
+#pragma unroll
+    for (int i = 0; i < 2 * NE; ++i) y[i] = to_float_odd(x[i] * f);
+    store_keys<HD>(blk, L, y);
+  }
+  if (lane == 0) *scale = kv8_pow2(e);
+}
+
+template <typename T, int HD>
+OSP_DEV void append_values(const Kv8AppendArgs& a, int r0, int off, int n, int g, uint8_t* blk, float* scale, int lane) {
+  constexpr int ND = HD / 32;
+  const Lanes<HD> L(lane);
+  float x[4][2][ND];
+  float amax = 0.f;
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int t = 4 * L.q + i;
+    const bool mine = t >= off && t < off + n;
+#pragma unroll
+    for (int d = 0; d < ND; ++d) {
+      float f[2] = {0.f, 0.f};
+      if (mine) load_n<T, 2>(a.v, (long)(r0 + t - off) * a.ldv + (long)g * HD + 16 * (L.dh * ND + d) + 2 * L.a, a.ks, a.split, f);
+#pragma unroll
+      for (int o = 0; o < 2; ++o) {
+        if (!(fabsf(f[o]) < INFINITY)) {
+          f[o] = 0.f;
+          bad = true;
+        }
+        x[i][o][d] = f[o];
+        amax = fmaxf(amax, fabsf(f[o]));
+      }
+    }
+  }
+  if (bad && a.err) atomicOr(a.err, 1u << 6);
+  amax = wave_max(amax);
+  const int was = off > 0 ? exp_of(*scale) : kKv8MinExp;
+  const int e = max(scale_exp((double)amax), was);
+  // 2^-e in two factors: either may lie outside the floats
+  const float f0 = kv8_pow2(-e / 2), f1 = kv8_pow2(-e - (-e / 2));
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int o = 0; o < 2; ++o)
+#pragma unroll
+      for (int d = 0; d < ND; ++d) x[i][o][d] = x[i][o][d] * f0 * f1;
+  store_values<HD>(blk, L, off, off + n, kv8_pow2(max(was - e, -126)), off > 0 && e > was, x);
+  if (lane == 0) *scale = kv8_pow2(e);
+}
+
+// Queries: HPW heads a wavefront, HD / (2 V) lanes a head, V values of either half a lane.
+template <typename T, int HD>
+OSP_DEV void do_queries(const Kv8AppendArgs& a, int row, int h0, int pos, int lane) {
+  constexpr int V = Vec<T>::N, LPH = HD / (2 * V);
+  const int h = h0 + lane / LPH, j = lane % LPH;
+  if (h >= a.nq) return;   // (whole groups of lanes that reduce together)
+  float x[2 * V];
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+    load_n<T, V>(a.q, (long)row * a.ldq + (long)h * HD + k * (HD / 2) + j * V, a.ks, a.split, x + k * V);
+  if (a.q_norm) {
+    float ss = 0.f;
+#pragma unroll
+    for (int i = 0; i < 2 * V; ++i) ss += x[i] * x[i];
+    ss += dpp_f<kDppXor1>(ss);
+    ss += dpp_f<kDppXor2>(ss);
+    if constexpr (LPH >= 8) ss += dpp_f<kDppHalfMirror>(ss);
+    if constexpr (LPH >= 16) ss += dpp_f<kDppMirror>(ss);
+    const float inv = 1.0f / sqrtf(ss / HD + a.eps);
+#pragma unroll
+    for (int i = 0; i < 2 * V; ++i) x[i] *= inv * gain(a.q_norm, a.g_bf16, (i / V) * (HD / 2) + j * V + i % V);
+  }
+  if (a.rope_cos) {
+    const long c = (long)min(max(pos, 0), a.max_pos - 1) * (HD / 2) + j * V;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const float co = a.rope_cos[c + i], si = a.rope_sin[c + i], u = x[i], w = x[V + i];
+      x[i] = u * co - w * si;
+      x[V + i] = w * co + u * si;
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    T* o = reinterpret_cast<T*>(a.q_out) + (long)row * a.ldo + (long)h * HD + k * (HD / 2) + j * V;
+    float* y = x + k * V;
+    if constexpr (sizeof(T) == 2) {
+      *reinterpret_cast<uint4*>(o) = make_uint4(f32x2_to_bf16x2(y[0] * a.q_scale, y[1] * a.q_scale), f32x2_to_bf16x2(y[2] * a.q_scale, y[3] * a.q_scale),
+                                                f32x2_to_bf16x2(y[4] * a.q_scale, y[5] * a.q_scale), f32x2_to_bf16x2(y[6] * a.q_scale, y[7] * a.q_scale));
+    } else {
+      *reinterpret_cast<float4*>(o) = make_float4(y[0] * a.q_scale, y[1] * a.q_scale, y[2] * a.q_scale, y[3] * a.q_scale);
+    }
+  }
+}
+
+// Wavefronts [0, units): blocks of the cache; the rest: queries.
+template <typename T, int HD>
+__global__ void __launch_bounds__(256) k_kv8_append(Kv8AppendArgs a, int units, int q_per_row) {
+  const int lane = threadIdx.x & 63;
+  const int w = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+  if (w < units) {
+    // kind and head innermost: the wavefronts of a page's rows run together
+    const int kind = w & 1, g = (w >> 1) % a.pool.nkv, u = (w >> 1) / a.pool.nkv;
+    const int b = unit_seq(a.r, u);
+    const Kv8Seq s = kv8_seq(a.r, b);
+    if (s.end <= s.beg) return;
+    const int pg = s.first / kKv8Page + u - (a.r.cu ? a.r.cu[b] / 16 + 2 * b : b);
+    const int lo = max(s.first, pg * kKv8Page), hi = min(s.first + (s.end - s.beg), (pg + 1) * kKv8Page);
+    if (lo >= hi) return;
+    const int id = kv8_page(a.pool, b, pg);
+    if (id < 0) {
+      if (lane == 0 && a.err) atomicOr(a.err, 1u << 3);
+      return;
+    }
+    uint8_t* blk = a.pool.codes + (long)id * a.pool.page_stride + ((long)kind * a.pool.nkv + g) * (kKv8Page * HD);
+    float* sc = a.pool.scales + (long)id * a.pool.scale_stride + 2 * g + kind;
+    const int off = lo - pg * kKv8Page, r0 = s.beg + lo - s.first;
+    if (kind == 0) append_keys<T, HD>(a, b, s, r0, off, hi - lo, g, blk, sc, lane);
+    else append_values<T, HD>(a, r0, off, hi - lo, g, blk, sc, lane);
+    return;
+  }
+  const int v = w - units;
+  const int row = v / q_per_row, h0 = (v % q_per_row) * (64 / (HD / (2 * Vec<T>::N)));
+  const int total = a.r.count ? min(*a.r.count, a.r.rows) : a.r.rows;
+  if (row >= total || (a.r.cu && row >= a.r.cu[a.r.B])) return;   // behind the last sequence
+  int pos = 0;
+  if (a.rope_cos) {
+    if (a.rope_pos) pos = a.rope_pos[row];
+    else if (a.r.pos) pos = a.r.pos[row];
+    else if (!a.r.cu) pos = a.r.cached[row];
+    else {
+      int lo = 0, hi = a.r.B - 1;   // the last sequence that begins at or before the row
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (a.r.cu[mid] <= row) lo = mid;
+        else hi = mid - 1;
+      }
+      pos = a.r.cached[lo] + row - a.r.cu[lo];
+    }
+  }
+  do_queries<T, HD>(a, row, h0, pos, lane);
+}
+
+// One wavefront per (sequence, kv head, keys or values): the positions base .. base + n - 1 take
+// the codes of base + path[i], page after page.  path ascends, so a position's source lies at or
+// behind it: reading a page's sources before writing it, in ascending order, moves in place.
+template <int HD>
+__global__ void __launch_bounds__(64) k_kv8_keep(Kv8KeepArgs a) {
+  constexpr int NE = HD / 8, ND = HD / 32;
+  const int lane = threadIdx.x, b = blockIdx.x, g = blockIdx.y >> 1, kind = blockIdx.y & 1;
+  const Lanes<HD> L(lane);
+  const int base = a.base[b], n = min(a.n[b], a.ld);
+  const int32_t* path = a.path + (long)b * a.ld;
+  if (n <= 0 || base < 0) return;
+  auto block = [&](int id) { return a.pool.codes + (long)id * a.pool.page_stride + ((long)kind * a.pool.nkv + g) * (kKv8Page * HD); };
+  auto scale = [&](int id) { return a.pool.scales + (long)id * a.pool.scale_stride + 2 * g + kind; };
+  for (int pg = base / kKv8Page; pg * kKv8Page < base + n; ++pg) {
+    const int lo = max(base, pg * kKv8Page), hi = min(base + n, (pg + 1) * kKv8Page), off = lo - pg * kKv8Page;
+    const int id = kv8_page(a.pool, b, pg);
+    // source of position pg * 16 + t: its page, token there, and whether it is one
+    auto source = [&](int t, int& tok) {
+      const int i = pg * kKv8Page + t - base;
+      if (i < 0 || i >= n) return -2;
+      const int at = path[i];
+      if (at < i || (i > 0 && path[i - 1] >= at)) return -1;
+      tok = (base + at) % kKv8Page;
+      return kv8_page(a.pool, b, (base + at) / kKv8Page);
+    };
+    bool bad = id < 0;
+    double amax = 0.0;
+    float x[2 * NE];                 // keys
+    float y[4][2][ND];               // values
+    if (kind == 0) {
+      int tok = 0;
+      const int src = source(L.t, tok);
+      bad |= src == -1;
+#pragma unroll
+      for (int i = 0; i < 2 * NE; ++i) x[i] = 0.f;
+      if (src >= 0) {
+        const float f = *scale(src);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const uint32_t* p = reinterpret_cast<const uint32_t*>(block(src) + tok * HD + h * (HD / 2) + L.j * NE);
+#pragma unroll
+          for (int i = 0; i < NE / 4; ++i) unpack4(p[i], x + h * NE + 4 * i);
+        }
+#pragma unroll
+        for (int i = 0; i < 2 * NE; ++i) {
+          x[i] *= f;
+          amax = fmax(amax, (double)fabsf(x[i]));
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        int tok = 0;
+        const int src = source(4 * L.q + i, tok);
+        bad |= src == -1;
+        const float f = src >= 0 ? *scale(src) : 0.f;
+        const uint8_t* p = block(max(src, 0)) + (tok / 4) * 4 * HD + tok % 4;
+#pragma unroll
+        for (int o = 0; o < 2; ++o)
+#pragma unroll
+          for (int d = 0; d < ND; ++d) {
+            float v = 0.f;
+            if (src >= 0) v = __builtin_amdgcn_cvt_f32_fp8((int)p[(2 * L.a + o) * (HD / 4) + (L.dh * ND + d) * 4], 0) * f;
+            y[i][o][d] = v;
+            amax = fmax(amax, (double)fabsf(v));
+          }
+      }
+    }
+    // (a page without a place, or a path that does not ascend: this sequence's move ends here)
+    if (__builtin_amdgcn_ballot_w64(bad)) {
+      if (lane == 0 && a.err) atomicOr(a.err, 1u << 3);
+      return;
+    }
+    amax = wave_max_d(amax);
+    const int was = off > 0 ? exp_of(*scale(id)) : kKv8MinExp;
+    const int e = max(scale_exp(amax), was);
+    const float f0 = kv8_pow2(-e / 2), f1 = kv8_pow2(-e - (-e / 2)), older = kv8_pow2(max(was - e, -126));
+    if (kind == 0) {
+      if (off > 0 && e > was) shift_keys<HD>(block(id), L, off, older);
+#pragma unroll
+      for (int i = 0; i < 2 * NE; ++i) x[i] = x[i] * f0 * f1;
+      if (L.t >= off && L.t < off + hi - lo) store_keys<HD>(block(id), L, x);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int o = 0; o < 2; ++o)
+#pragma unroll
+          for (int d = 0; d < ND; ++d) y[i][o][d] = y[i][o][d] * f0 * f1;
+      store_values<HD>(block(id), L, off, off + hi - lo, older, off > 0 && e > was, y);
+    }
+    if (lane == 0) *scale(id) = kv8_pow2(e);
+  }
+}
+
+}  // namespace
+
+void launch_kv8_append(const Kv8AppendArgs& a, hipStream_t st) {
+  const int pages = a.r.cu ? a.r.rows / 16 + 2 * a.r.B : a.r.B;
+  const int units = pages * a.pool.nkv * 2;
+  const int hpw = 64 / (a.hd / (2 * (a.x_bf16 ? 8 : 4)));
+  const int q_per_row = a.q ? (a.nq + hpw - 1) / hpw : 1;
+  const long waves = units + (a.q ? (long)a.r.rows * q_per_row : 0);
+  const dim3 grid((unsigned)((waves + 3) / 4));
+  if (a.x_bf16) {
+    if (a.hd == 128) hipLaunchKernelGGL((k_kv8_append<bf16_t, 128>), grid, dim3(256), 0, st, a, units, q_per_row);
+    else hipLaunchKernelGGL((k_kv8_append<bf16_t, 64>), grid, dim3(256), 0, st, a, units, q_per_row);
+  } else {
+    if (a.hd == 128) hipLaunchKernelGGL((k_kv8_append<float, 128>), grid, dim3(256), 0, st, a, units, q_per_row);
+    else hipLaunchKernelGGL((k_kv8_append<float, 64>), grid, dim3(256), 0, st, a, units, q_per_row);
+  }
+}
+
+void launch_kv8_keep(const Kv8KeepArgs& a, hipStream_t st) {
+  const dim3 grid(a.B, 2 * a.pool.nkv);
+  if (a.hd == 128) hipLaunchKernelGGL(k_kv8_keep<128>, grid, dim3(64), 0, st, a);
+  else hipLaunchKernelGGL(k_kv8_keep<64>, grid, dim3(64), 0, st, a);
+}
+
+}  // namespace osp

@@ -1,0 +1,521 @@
+"""The 8-bit cache on the GPU against its float64 description (kv8_ref): codes and scales
+equal, attention within the roundings that its types make."""
+import math
+import random
+
+import pytest
+import torch
+
+from . import kv8_ref as R
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+BF, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+
+
+def bd():
+    from paper_2609_09338_amd import binding
+    return binding
+
+
+def ints(x):
+    return torch.tensor(x, dtype=torch.int32, device=DEV)
+
+
+def make_cache(batch, max_pages, nkv, hd, seed, layers=1, poison=True):
+    """A pool with shuffled pages whose memory is NaN codes and NaN scales until written."""
+    rng = random.Random(seed)
+    pages = batch * max_pages + 3
+    codes = torch.full((pages, layers, 2, nkv, 16 * hd), 0x7F if poison else 0, dtype=torch.uint8, device=DEV)
+    scales = torch.full((pages, layers, nkv, 2), math.nan if poison else 1.0, dtype=F32, device=DEV)
+    ids = list(range(pages))
+    rng.shuffle(ids)
+    table = ints([[ids[b * max_pages + p] for p in range(max_pages)] for b in range(batch)])
+    return bd().Kv8Cache(codes[:, layers - 1], scales[:, layers - 1], table, hd)
+
+
+def fill(cache, lengths, gen, key_scale=1.0, value_scale=1.0):
+    """Appends `lengths` random positions."""
+    n = sum(lengths)
+    if n == 0:
+        return
+    k = torch.randn((n, cache.n_kv_heads, cache.head_dim), generator=gen, device=DEV) * key_scale
+    v = torch.randn((n, cache.n_kv_heads, cache.head_dim), generator=gen, device=DEV) * value_scale
+    bd().kv8_append(cache, k, v, ints([0] * len(lengths)), cu_rows=ints([0] + list(torch.tensor(lengths).cumsum(0))))
+
+
+def cu_of(rows):
+    return [0] + torch.tensor(rows).cumsum(0).tolist()
+
+
+def ref_of(cache):
+    return R.Cache(torch.nan_to_num(cache.codes.contiguous().view(torch.float8_e4m3fn).float(), nan=0.0).to(torch.float8_e4m3fn)
+                   .view(torch.uint8), torch.nan_to_num(cache.scales, nan=1.0), cache.page_table, cache.head_dim)
+
+
+def tables(n, hd, theta=1e6):
+    ang = torch.arange(n, dtype=torch.float64)[:, None] * theta ** (-torch.arange(hd // 2, dtype=torch.float64) * 2 / hd)
+    return ang.cos().float(), ang.sin().float()
+
+
+def gen_of(seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    return g
+
+
+def same_cache(cache, ref, b, n):
+    """The first n positions of sequence b: codes' values and scales, exactly."""
+    got = ref_of(cache)
+    pages = ref.table[b, :(n + 15) // 16]
+    for i, p in enumerate(pages.tolist()):
+        live = min(16, n - 16 * i)
+        assert torch.equal(got.s[p], ref.s[p]), f"sequence {b} page {i}: scales"
+        d = (got.v[p, :, :, :live] != ref.v[p, :, :, :live]).sum()
+        assert int(d) == 0, f"sequence {b} page {i}: {int(d)} codes differ"
+
+
+APPEND = [
+    # heads, type, cached lengths, rows, gains, rotation
+    ((4, 4, 64), F32, [0], [1], True, True),
+    ((16, 8, 128), BF, [0, 15, 16, 17], [1, 1, 1, 1], True, True),
+    ((16, 8, 128), BF, [5, 0, 31, 40], [37, 1, 0, 18], True, True),
+    ((32, 8, 64), BF, [3, 250], [64, 33], False, True),
+    ((32, 8, 128), F32, [9], [200], True, False),
+    ((5, 1, 64), F32, [0, 1, 2], [16, 15, 31], False, False),
+    ((3, 3, 128), BF, [12] * 70, [3] * 70, True, True),
+]
+
+
+@pytest.mark.parametrize("heads,dtype,cached,rows,gains,rope", APPEND)
+def test_append_writes_the_codes_of_the_definition(heads, dtype, cached, rows, gains, rope):
+    nq, nkv, hd = heads
+    B, n = len(rows), sum(rows)
+    gen = gen_of(hash((heads, n)) % 1000)
+    cache = make_cache(B, (max(c + r for c, r in zip(cached, rows)) + 15) // 16, nkv, hd, 3, layers=2)
+    fill(cache, cached, gen, key_scale=0.3)
+    ref = ref_of(cache)
+    # rows within a wider product, and rows behind the last sequence
+    x = torch.randn((n + 2, (nq + 2 * nkv) * hd + 16), generator=gen, device=DEV) * torch.exp(
+        torch.randn((n + 2, 1), generator=gen, device=DEV) * 1.5)
+    x = x.to(dtype)
+    q, k, v = x[:, :(nq + 2 * nkv) * hd].unflatten(1, (nq + 2 * nkv, hd)).split((nq, nkv, nkv), 1)
+    g = [(1 + 0.2 * torch.randn(hd, generator=gen, device=DEV)).to(dtype) if gains else None for _ in range(2)]
+    cos, sin = tables(max(c + r for c, r in zip(cached, rows)), hd)
+    out = torch.full((n + 2, nq, hd), 7.0, dtype=dtype, device=DEV)
+    err = ints([0])
+    kw = dict(rope_cos=cos.to(DEV), rope_sin=sin.to(DEV)) if rope else {}
+    bd().kv8_append(cache, k, v, ints(cached), q=q, q_out=out, cu_rows=ints(cu_of(rows)), q_norm=g[0], k_norm=g[1], errors=err, **kw)
+    torch.cuda.synchronize()
+    assert int(err) == 0
+    r0 = 0
+    half = 2.0 ** -8 if dtype == BF else 2.0 ** -24
+    for b, (c, r) in enumerate(zip(cached, rows)):
+        if r:
+            at = torch.arange(c, c + r)
+            cs = (cos[at], sin[at]) if rope else (None, None)
+            cpu = lambda t: None if t is None else t.cpu()  # noqa: E731
+            kr = R.norm_rope(k[r0:r0 + r].cpu().double(), cpu(g[1]), 1e-6, *cs)
+            ref.write(b, c, kr, v[r0:r0 + r].cpu().double())
+            qr = R.norm_rope(q[r0:r0 + r].cpu().double(), cpu(g[0]), 1e-6, *cs)
+            # a sum of hd squares, a root, a quotient, two gains, two products: fp32
+            big = torch.maximum(qr.abs(), qr.roll(hd // 2, -1).abs())
+            tol = half * qr.abs() + (hd + 16) * 2.0 ** -24 * big * 2 ** 0.5 * 2
+            assert bool(((out[r0:r0 + r].cpu().double() - qr).abs() <= tol).all())
+        same_cache(cache, ref, b, c + r)
+        r0 += r
+    if any(r != 1 for r in rows):
+        assert bool((out[n:] == 7.0).all()), "rows behind the last sequence were written"
+
+
+def test_append_token_by_token_grows_scales_as_one_call_each():
+    """Forty calls of one row each, magnitudes rising and falling by powers of two."""
+    nkv, hd = 2, 64
+    gen = gen_of(5)
+    cache = make_cache(2, 4, nkv, hd, 8)
+    ref = ref_of(cache)
+    for t in range(40):
+        f = 2.0 ** [0, 3, -9, 12, -14, 1, 18][t % 7]
+        k, v = (torch.randn((2, nkv, hd), generator=gen, device=DEV) * f for _ in range(2))
+        bd().kv8_append(cache, k, v, ints([t, t]))
+        for b in range(2):
+            ref.write(b, t, k[b:b + 1].cpu().double(), v[b:b + 1].cpu().double())
+    for b in range(2):
+        same_cache(cache, ref, b, 40)
+
+
+def test_append_after_a_rollback_keeps_the_scale_within_a_page_and_drops_it_at_the_next():
+    nkv, hd = 1, 128
+    cache = make_cache(1, 3, nkv, hd, 9)
+    ref = ref_of(cache)
+    for t0, n, f in ((0, 20, 1.0), (10, 6, 1e-3), (16, 8, 1e-3), (3, 30, 50.0)):
+        k, v = (torch.randn((n, nkv, hd), generator=gen_of(t0), device=DEV) * f for _ in range(2))
+        bd().kv8_append(cache, k, v, ints([t0]), cu_rows=ints([0, n]))
+        ref.write(0, t0, k.cpu().double(), v.cpu().double())
+        same_cache(cache, ref, 0, t0 + n)
+
+
+def test_append_zeros_extremes_and_values_that_are_not_finite():
+    nkv, hd = 1, 64
+    cache = make_cache(1, 8, nkv, hd, 4)
+    ref = ref_of(cache)
+    x = torch.randn((96, nkv, hd), generator=gen_of(1), device=DEV)
+    x[:16] = 0.0
+    x[16:32] *= 1e-36
+    x[32:48] = 448.0 * 2.0 ** 5            # exactly at a scale's border
+    x[48:64] *= 3e37
+    x[64:80] = 448.0 * 2.0 ** 5 * (1 + 2.0 ** -23)   # just past it
+    x[80, 0, 0], x[81, 0, 3], x[82, 0, 63] = math.inf, math.nan, -math.inf
+    err = ints([0])
+    bd().kv8_append(cache, x, x, ints([0]), cu_rows=ints([0, 96]), errors=err)
+    ref.write(0, 0, x.cpu().double(), x.cpu().double())
+    same_cache(cache, ref, 0, 96)
+    assert int(err) == 1 << 6
+    assert float(ref.s[int(cache.page_table[0, 2].cpu()), 0, 0]) == 32.0
+    assert float(ref.s[int(cache.page_table[0, 4].cpu()), 0, 0]) == 64.0
+
+
+def test_append_ties_round_to_even_and_keys_round_once():
+    """Values midway between codes, and a double's distance beside them."""
+    nkv, hd = 1, 64
+    tab = R.e4m3_values()
+    mid = (tab[1:] + tab[:-1]) / 2
+    x = torch.zeros((16, hd), dtype=torch.float64)
+    x.view(-1)[:126] = mid
+    x.view(-1)[126:252] = -mid
+    x[:, hd - 1] = 448.0                     # scale 1
+    x = x.float().to(DEV)[:, None]
+    cache = make_cache(1, 1, nkv, hd, 4)
+    ref = ref_of(cache)
+    bd().kv8_append(cache, x, x, ints([0]), cu_rows=ints([0, 16]))
+    ref.write(0, 0, x.cpu().double(), x.cpu().double())
+    same_cache(cache, ref, 0, 16)
+    # rotated by an angle whose cosine is a float below one: a little under the middle
+    cos = torch.full((16, hd // 2), 1.0 - 2.0 ** -24, device=DEV)
+    sin = torch.zeros((16, hd // 2), device=DEV)
+    bd().kv8_append(cache, x, x, ints([0]), cu_rows=ints([0, 16]), rope_cos=cos, rope_sin=sin)
+    ref.write(0, 0, x.cpu().double() * float(cos[0, 0]), x.cpu().double())
+    same_cache(cache, ref, 0, 16)
+
+
+def test_append_beyond_the_pages_is_skipped_and_reported():
+    nkv, hd = 2, 64
+    cache = make_cache(2, 2, nkv, hd, 4)
+    before = cache.codes.clone()
+    cache.page_table[1, 0] = 1 << 20       # not a page of the pool
+    k = torch.randn((12, nkv, hd), generator=gen_of(1), device=DEV)
+    err = ints([0])
+    bd().kv8_append(cache, k, k, ints([30, 2]), cu_rows=ints([0, 8, 12]), errors=err)
+    torch.cuda.synchronize()
+    assert int(err) == 1 << 3
+    ids = cache.page_table.cpu()
+    got = cache.codes.clone()
+    last = int(ids[0, 1])
+    assert not torch.equal(got[last], before[last])      # positions 30 and 31 are written
+    got[last] = before[last]
+    assert torch.equal(got, before)
+    out = torch.empty((12, 4, hd), dtype=F32, device=DEV)
+    cos, sin = (t.to(DEV) for t in tables(10, hd))
+    err.zero_()
+    bd().kv8_append(cache, k, k, ints([0, 16]), q=torch.zeros_like(out), q_out=out, cu_rows=ints([0, 12, 12]), rope_cos=cos, rope_sin=sin,
+                    errors=err)
+    assert int(err) == 1 << 7              # positions 10 and 11 have no angles
+
+
+ATTEND = [
+    # heads, type, cached, rows, key scale
+    ((4, 4, 64), F32, [0], [1], 1.0),
+    ((4, 4, 64), F32, [127], [1], 1.0),
+    ((16, 8, 128), BF, [2047], [1], 1.0),
+    ((16, 8, 128), BF, [0, 1, 15, 16, 33, 127, 128, 900], [1] * 8, 3.0),
+    ((16, 8, 128), F32, [700, 3], [8, 5], 1.0),
+    ((32, 8, 64), BF, [511, 40, 0], [7, 0, 1], 1.0),
+    ((32, 8, 128), BF, [60, 1030], [9, 17], 1.0),
+    ((32, 8, 128), F32, [100], [33], 2.0),
+    ((6, 1, 64), BF, [3], [50], 1.0),
+    ((48, 1, 64), BF, [77], [3], 1.0),
+    ((2, 2, 128), BF, [0, 90], [300, 77], 1.0),
+    ((8, 2, 64), F32, [0], [257], 1.0),
+    ((8, 8, 128), BF, [5] * 67, [1] * 67, 1.0),
+    ((4, 2, 128), BF, [30000, 50], [1, 1], 1.0),
+    ((4, 2, 64), F32, [20000, 9000], [2, 3], 1.0),
+]
+
+
+def check_attention(cache, cached, rows, dtype, gen, nq, q_scale=1.3, masks=None, max_context=None, ref=None, scale=None):
+    hd, n = cache.head_dim, sum(rows)
+    q = (torch.randn((n + 1, nq + 1, hd), generator=gen, device=DEV) * q_scale).to(dtype)[:, :nq]   # strided rows
+    out = torch.full((n + 1, nq + 2, hd), 7.0, dtype=dtype, device=DEV)[:, 1:nq + 1]
+    ctx = max_context or max(c + r for c, r in zip(cached, rows))
+    ws = torch.empty(bd().kv8_attention_workspace(cache, n + 1, nq, max(rows), ctx), dtype=torch.uint8, device=DEV)
+    err = ints([0])
+    tree = None
+    if masks is not None:
+        words = [[(w >> 64 * i) & (1 << 64) - 1 for i in (0, 1)] for m in masks for w in m] + [[0, 0]]
+        tree = torch.tensor([[w - (1 << 64) if w >> 63 else w for w in r] for r in words], dtype=torch.int64, device=DEV)
+    bd().kv8_attention(cache, q, out, ints(cached), ws, max_rows=max(rows), max_context=ctx, cu_rows=ints(cu_of(rows)), tree_mask=tree,
+                       errors=err, scale=scale)
+    torch.cuda.synchronize()
+    assert int(err) == 0
+    assert bool((out[n:] == 7.0).all()), "a row behind the last sequence was written"
+    ref = ref or ref_of(cache)
+    r0, worst = 0, 0.0
+    for b, (c, r) in enumerate(zip(cached, rows)):
+        if r == 0:
+            continue
+        sees = torch.arange(c + r)[None] <= torch.arange(c, c + r)[:, None]
+        if masks is not None:
+            new = torch.tensor([[bool(w >> i & 1) for i in range(r)] for w in masks[b]])
+            sees = torch.cat([torch.ones((r, c), dtype=torch.bool), new], 1)
+        o, tol = R.attention(ref, b, q[r0:r0 + r].cpu(), sees, hd ** -0.5 if scale is None else scale, 2.0 ** -11 if dtype == BF else 2.0 ** -22,
+                             2.0 ** -8 if dtype == BF else 2.0 ** -24)
+        d = (out[r0:r0 + r].cpu().double() - o).abs()
+        assert bool((d <= tol).all()), f"sequence {b}: off by {float((d - tol).max()):.3g} more than {float(tol.max()):.3g}"
+        worst = max(worst, float((d / tol.clamp(min=1e-30)).max()))
+        r0 += r
+    return out
+
+
+@pytest.mark.parametrize("heads,dtype,cached,rows,key_scale", ATTEND)
+def test_attention_equals_the_definition(heads, dtype, cached, rows, key_scale):
+    nq, nkv, hd = heads
+    gen = gen_of(len(rows) + hd)
+    cache = make_cache(len(rows), (max(c + r for c, r in zip(cached, rows)) + 15) // 16 + 1, nkv, hd, 7, layers=2)
+    fill(cache, [c + r for c, r in zip(cached, rows)], gen, key_scale=key_scale)
+    check_attention(cache, cached, rows, dtype, gen, nq)
+
+
+@pytest.mark.parametrize("max_context", [1, 100, 100000])
+def test_attention_is_right_whatever_context_it_was_planned_for(max_context):
+    cached, rows = [3000, 10, 700], [1, 2, 1]
+    cache = make_cache(3, 190, 2, 64, 7)
+    fill(cache, [c + r for c, r in zip(cached, rows)], gen_of(3))
+    check_attention(cache, cached, rows, BF, gen_of(4), 4, max_context=max_context)
+
+
+def random_masks(rows, rng, empty=0.1):
+    out = []
+    for n in rows:
+        m = []
+        for i in range(n):
+            up = rng.choice(m + [0])
+            m.append(0 if rng.random() < empty else up | 1 << i)
+        out.append(m)
+    return out
+
+
+@pytest.mark.parametrize("heads,dtype,cached,rows", [
+    ((32, 8, 64), BF, [300, 1000, 0], [33, 65, 65]),
+    ((16, 8, 128), F32, [17, 0], [16, 128]),
+    ((4, 4, 64), BF, [0, 64, 127], [1, 5, 100]),
+])
+def test_attention_with_tree_masks_and_rows_that_see_nothing(heads, dtype, cached, rows):
+    nq, nkv, hd = heads
+    gen, rng = gen_of(11), random.Random(6)
+    cache = make_cache(len(rows), (max(c + r for c, r in zip(cached, rows)) + 15) // 16, nkv, hd, 7)
+    fill(cache, [c + r for c, r in zip(cached, rows)], gen)
+    masks = random_masks(rows, rng)
+    out = check_attention(cache, cached, rows, dtype, gen, nq, masks=masks)
+    r0 = cu_of(rows)
+    empty = [r0[b] + i for b, m in enumerate(masks) if cached[b] == 0 for i, w in enumerate(m) if w == 0]
+    if empty:
+        assert bool((out[empty] == 0).all())
+
+
+def test_attention_of_sharp_scores_and_of_blocks_of_very_different_scales():
+    nkv, hd = 2, 128
+    gen = gen_of(21)
+    cache = make_cache(1, 40, nkv, hd, 7)
+    n = 600
+    k = torch.randn((n, nkv, hd), generator=gen, device=DEV)
+    v = torch.randn((n, nkv, hd), generator=gen, device=DEV)
+    f = 2.0 ** (torch.arange(n, device=DEV) // 16 % 9 * 3.0 - 12)     # from page to page
+    v = v * f[:, None, None]
+    v[128:160] = 0.0                                                  # pages of zeros
+    bd().kv8_append(cache, k, v, ints([0]), cu_rows=ints([0, n]))
+    for dtype in (BF, F32):
+        check_attention(cache, [n - 3], [3], dtype, gen, 4)
+        check_attention(cache, [n - 3], [3], dtype, gen, 4, q_scale=40.0)   # nearly one-hot
+        check_attention(cache, [n - 200], [200], dtype, gen, 4, q_scale=8.0)
+        check_attention(cache, [n - 3], [3], dtype, gen, 4, scale=1e-3)
+
+
+def test_attention_with_a_first_position_that_takes_most_of_the_weight():
+    """The rest weighs 2^-13 a token and more than it in sum: probabilities far below the maximum count."""
+    nkv, hd, n = 1, 64, 40000
+    cache = make_cache(1, n // 16 + 1, nkv, hd, 7)
+    gen = gen_of(2)
+    k = torch.randn((n, nkv, hd), generator=gen, device=DEV) * 1e-3
+    k[0] = 13.0 * math.log(2.0) / math.sqrt(hd)
+    v = torch.randn((n, nkv, hd), generator=gen, device=DEV) + 1.0
+    v[0] = -1.0
+    bd().kv8_append(cache, k, v, ints([0]), cu_rows=ints([0, n]))
+    q = torch.ones((1, 1, hd), dtype=F32, device=DEV)
+    out = torch.empty_like(q)
+    ws = torch.empty(bd().kv8_attention_workspace(cache, 1, 1, 1, n), dtype=torch.uint8, device=DEV)
+    bd().kv8_attention(cache, q, out, ints([n - 1]), ws, max_context=n)
+    o, tol = R.attention(ref_of(cache), 0, q.cpu(), torch.ones((1, n), dtype=torch.bool), hd ** -0.5, 2.0 ** -22, 2.0 ** -24)
+    assert bool(((out.cpu().double() - o).abs() <= tol).all())
+
+
+def test_attention_reports_positions_without_a_page():
+    nkv, hd = 2, 64
+    cache = make_cache(2, 4, nkv, hd, 4)
+    fill(cache, [64, 64], gen_of(1))
+    cache.page_table[0, 1] = -1
+    q = torch.randn((2, 4, hd), generator=gen_of(2), device=DEV)
+    out = torch.empty_like(q)
+    ws = torch.empty(bd().kv8_attention_workspace(cache, 2, 4, 1, 64), dtype=torch.uint8, device=DEV)
+    err = ints([0])
+    bd().kv8_attention(cache, q, out, ints([63, 39]), ws, max_context=64, errors=err)
+    torch.cuda.synchronize()
+    assert int(err) == 1 << 2 and bool(torch.isfinite(out).all())
+    err.zero_()
+    cache.page_table[0, 1] = cache.page_table[0, 0]
+    bd().kv8_attention(cache, q, out, ints([64, 2000000000]), ws, max_context=64, errors=err)   # past the table
+    torch.cuda.synchronize()
+    assert int(err) == 1 << 2 and bool(torch.isfinite(out).all())
+
+
+@pytest.mark.parametrize("hd,nkv,base,paths", [
+    (64, 4, [20], [[0, 2, 3, 7]]),
+    (128, 8, [0, 15, 16, 100, 7], [[1, 2], [0, 1, 2], [5, 9, 30, 41], [], [63]]),
+    (128, 2, [3, 9], [list(range(40)), list(range(0, 60, 2))]),
+])
+def test_keep_moves_an_accepted_path(hd, nkv, base, paths):
+    B, N = len(base), 64
+    gen = gen_of(31)
+    cache = make_cache(B, (max(base) + N + 15) // 16, nkv, hd, 5)
+    n = sum(b + N for b in base)
+    k = torch.randn((n, nkv, hd), generator=gen, device=DEV) * torch.exp(torch.randn((n, nkv, 1), generator=gen, device=DEV))
+    v = torch.randn((n, nkv, hd), generator=gen, device=DEV) * torch.exp(torch.randn((n, nkv, 1), generator=gen, device=DEV))
+    bd().kv8_append(cache, k, v, ints([0] * B), cu_rows=ints(cu_of([b + N for b in base])))
+    ref = ref_of(cache)
+    err = ints([0])
+    bd().kv8_keep(cache, ints(base), ints([p + [-1] * (N - len(p)) for p in paths]), ints([len(p) for p in paths]), errors=err)
+    for b, p in enumerate(paths):
+        ref.keep(b, base[b], p)
+        same_cache(cache, ref, b, base[b] + len(p))
+    assert int(err) == 0
+
+
+def test_keep_refuses_a_path_that_does_not_ascend():
+    cache = make_cache(2, 4, 1, 64, 5)
+    fill(cache, [64, 64], gen_of(1))
+    ref = ref_of(cache)
+    err = ints([0])
+    bd().kv8_keep(cache, ints([4, 4]), ints([[3, 2, 9], [0, 5, 9]]), ints([3, 2]), errors=err)
+    ref.keep(1, 4, [0, 5])
+    same_cache(cache, ref, 0, 64)
+    same_cache(cache, ref, 1, 6)
+    assert int(err) == 1 << 3
+
+
+def test_a_tree_verified_kept_and_continued():
+    """A layer's calls as a target makes them: prompt, tree rows, their mask, the accepted path, the
+    next token; every attention against the reference cache that went through the same steps."""
+    nq, nkv, hd, B = 8, 2, 64, 2
+    gen = gen_of(41)
+    cache = make_cache(B, 12, nkv, hd, 5)
+    ref = ref_of(cache)
+    cos, sin = tables(200, hd)
+    gain = (1 + 0.1 * torch.randn(hd, generator=gen, device=DEV)).to(BF)
+
+    def step(cached, rows, pos=None, masks=None):
+        n = sum(rows)
+        x = torch.randn((n, nq + 2 * nkv, hd), generator=gen, device=DEV).to(BF)
+        q, k, v = x.split((nq, nkv, nkv), 1)
+        at = torch.cat([torch.arange(c, c + r) for c, r in zip(cached, rows)]) if pos is None else torch.tensor(pos)
+        bd().kv8_append(cache, k, v, ints(cached), q=q, q_out=q, cu_rows=ints(cu_of(rows)), q_norm=gain, k_norm=gain,
+                        rope_pos=None if pos is None else ints(pos), rope_cos=cos.to(DEV), rope_sin=sin.to(DEV))
+        r0 = 0
+        for b, (c, r) in enumerate(zip(cached, rows)):
+            kr = R.norm_rope(k[r0:r0 + r].cpu().double(), gain.cpu(), 1e-6, cos[at[r0:r0 + r]], sin[at[r0:r0 + r]])
+            if r:
+                ref.write(b, c, kr, v[r0:r0 + r].cpu().double())
+            same_cache(cache, ref, b, c + r)
+            r0 += r
+        check_attention(cache, cached, rows, BF, gen, nq, masks=masks, ref=ref)
+
+    step([0, 0], [70, 19])
+    # root, two children, a child of each, a grandchild
+    parents = [-1, 0, 0, 1, 2, 4]
+    mask, depth = [], []
+    for i, p in enumerate(parents):
+        mask.append((mask[p] if p >= 0 else 0) | 1 << i)
+        depth.append(depth[p] + 1 if p >= 0 else 0)
+    step([70, 19], [6, 6], pos=[c + d for c in (70, 19) for d in depth], masks=[mask, mask])
+    paths = [[2, 4, 5], [1]]
+    bd().kv8_keep(cache, ints([71, 20]), ints([[p - 1 for p in path] + [-1] * (5 - len(path)) for path in paths]), ints([3, 1]))
+    for b, (c, path) in enumerate(zip((71, 20), paths)):
+        ref.keep(b, c, [p - 1 for p in path])
+        same_cache(cache, ref, b, c + len(path))
+    step([74, 21], [1, 1])
+    step([75, 22], [5, 40])
+
+
+def test_captured_calls_follow_lengths_and_inputs_on_replay():
+    """append and attention recorded once; lengths and rows change between replays, with eager
+    work of the same kind in between, each replay equal to the eager calls bit for bit."""
+    nq, nkv, hd, B = 8, 2, 128, 3
+    gen = gen_of(51)
+    cached = [500, 20, 130]
+    cache = make_cache(B, 60, nkv, hd, 5)
+    fill(cache, cached, gen)
+    other = make_cache(B, 60, nkv, hd, 5)
+    other.codes.copy_(cache.codes)
+    other.scales.copy_(cache.scales)
+    x = torch.empty((B, nq + 2 * nkv, hd), dtype=BF, device=DEV)
+    lens = ints(cached)
+    ws = [torch.empty(bd().kv8_attention_workspace(cache, B, nq, 1, 600), dtype=torch.uint8, device=DEV) for _ in range(2)]
+    outs = [torch.empty((B, nq, hd), dtype=BF, device=DEV) for _ in range(2)]
+    qs = [torch.empty((B, nq, hd), dtype=BF, device=DEV) for _ in range(2)]
+    cos, sin = (t.to(DEV) for t in tables(960, hd))
+
+    def layer(c, i):
+        q, k, v = x.split((nq, nkv, nkv), 1)
+        bd().kv8_append(c, k, v, lens, q=q, q_out=qs[i], rope_cos=cos, rope_sin=sin)
+        bd().kv8_attention(c, qs[i], outs[i], lens, ws[i], max_context=600)
+
+    s = torch.cuda.Stream()
+    x.copy_(torch.randn(x.shape, generator=gen, device=DEV))
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        layer(cache, 0)
+    for it in range(5):
+        x.copy_(torch.randn(x.shape, generator=gen, device=DEV))
+        g.replay()
+        layer(other, 1)
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0], outs[1]), it
+        assert torch.equal(cache.codes, other.codes)
+        lens += 1 if it % 2 else 70     # (a step, or as after a further prompt: positions in between hold old pages)
+        fill_more = torch.randn((B * 70, nkv, hd), generator=gen, device=DEV)
+        if it % 2 == 0:
+            for c in (cache, other):
+                bd().kv8_append(c, fill_more, fill_more, lens - 69, cu_rows=ints([0, 70, 140, 210]))
+
+
+def test_calls_on_another_stream_and_twice_give_the_same_bits():
+    nq, nkv, hd = 16, 8, 128
+    cached, rows = [3000, 500, 77], [4, 1, 9]
+    cache = make_cache(3, 190, nkv, hd, 7)
+    fill(cache, [c + r for c, r in zip(cached, rows)], gen_of(3))
+    q = torch.randn((14, nq, hd), generator=gen_of(4), device=DEV).to(BF)
+    outs = [torch.zeros_like(q) for _ in range(3)]
+    ws = [torch.empty(bd().kv8_attention_workspace(cache, 14, nq, 9, 3004), dtype=torch.uint8, device=DEV) for _ in range(3)]
+    args = dict(max_rows=9, max_context=3004, cu_rows=ints(cu_of(rows)))
+    lens = ints(cached)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.current_stream(), torch.cuda.Stream(), torch.cuda.Stream()]
+    for o, w, s in zip(outs, ws, streams):
+        bd().kv8_attention(cache, q, o, lens, w, stream=s, **args)
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
