@@ -21,7 +21,7 @@ BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libosprey.so")
 SOURCES = ["gemv.hip", "gemv_taps.hip", "gemv_qkv.hip", "gemv_resid.hip", "gemv_swiglu.hip",
            "gemv_logits.hip", "gemm_mfma.hip", "gemm_rows.hip", "skinny.hip", "rows.hip", "attention.hip", "attention_rows.hip", "sample.hip", "verify.hip", "verify_static.hip",
-           "state.hip", "tree.hip", "kv8_append.hip", "kv8_attention.hip", "osprey.cpp", "kv8.cpp"]
+           "state.hip", "tree.hip", "kv8_append.hip", "kv8_attention.hip", "kv8_prompt.hip", "osprey.cpp", "kv8.cpp"]
 ARCH = "gfx950"
 
 

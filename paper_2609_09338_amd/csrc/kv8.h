@@ -24,6 +24,7 @@ namespace osp {
 constexpr int kKv8Page = 16;
 constexpr int kKv8MinExp = -100;   // smallest scale 2^-100 (an all-zero block)
 constexpr int kKv8MaxExp = 120;    // 448 * 2^120 holds every finite float
+constexpr int kKv8MaxSplits = 64;  // splits of a context: a lane each in a join
 constexpr int kKv8MaxPos = 1 << 30;
 
 struct Kv8Pool {
@@ -106,8 +107,10 @@ struct Kv8AttnArgs {
   uint16_t *o_hi, *o_lo;    // or bf16 pairs [rows][nq hd] (nullable)
   uint32_t* err;
 };
-// Column tiles (16 nt query vectors each) per kv head of `rows` rows in B sequences: a bound.
-int kv8_attention_tiles(int rows, int B, int group, int max_rows);
+// Query vectors of one tile of a pass of at most max_rows rows a sequence.
+constexpr int kKv8PromptWaves = 4, kKv8PromptNt = 2, kKv8PromptCols = 16 * kKv8PromptNt * kKv8PromptWaves;
+int kv8_attention_cols(int x_bf16, int group, int max_rows);
+void launch_kv8_prompt(const Kv8AttnArgs& a, dim3 grid, hipStream_t st);
 void launch_kv8_attention(const Kv8AttnArgs& a, int max_rows, hipStream_t st);
 // out = the splits' joined outputs (a.n_split > 1)
 void launch_kv8_join(const Kv8AttnArgs& a, hipStream_t st);

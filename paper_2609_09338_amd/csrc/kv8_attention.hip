@@ -14,38 +14,19 @@
 //   * Queries are scaled by a power of two per vector into f16's range: bf16 queries are then
 //     exact (f16 keeps 11 bits), fp32 ones go in as hi + lo (22 bits, two products).
 //   * A key block's scale and the softmax scale are one factor of the exponent's fma.  A value
-//     block's scale, relative to the largest of the wavefront's pages, multiplies P as it is
-//     rounded to f16.  P is held with 2^6 .. 2^14 as its largest value: 11 bits down to 2^-20 of it
-//     and an absolute 2^-30 below, where bf16's 8 bits would add an error of the output's own
-//     rounding.  fp32 rows take P as hi + lo as well.  Maxima, sums and outputs are fp32.
+//     block's scale, relative to the largest of the wavefront's pages so far, is an operand of its
+//     codes' conversion.  P is held in f16 with 2^6 .. 2^14 as its largest value: 11 bits down to
+//     2^-20 of it and an absolute 2^-31 below, where bf16's 8 bits would add an error of the output's
+//     own rounding.  fp32 rows take P as hi + lo as well.  Maxima, sums and outputs are fp32.
 //   * The running maximum only moves when a score passes it by 2^8 (one ballot a pair, no
-//     cross-lane traffic otherwise); sums stay per lane until the end.
+//     cross-lane traffic otherwise), and then to a whole number: outputs are rescaled by powers of
+//     two, exactly.  Sums stay per lane until the end.
 #include <algorithm>
 
-#include "kv8.h"
+#include "kv8_attn.h"
 
 namespace osp {
 namespace {
-
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr float kNoMax = -1.0e30f;   // below any score: a row that has seen nothing
-constexpr float kLift = 6.f;         // P's largest value is 2^kLift, 2^(kLift + kSlack) before the maximum moves
-constexpr float kSlack = 8.f;
-
-OSP_DEV uint32_t h2(f16x2 v) { return __builtin_bit_cast(uint32_t, v); }
-OSP_DEV uint32_t codes_f16(uint32_t u, bool hi) {
-  return hi ? h2(__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(u, 1.f, true)) : h2(__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(u, 1.f, false));
-}
-OSP_DEV f16x8 frag(uint32_t a, uint32_t b, uint32_t c, uint32_t d) { return __builtin_bit_cast(f16x8, make_uint4(a, b, c, d)); }
-// Eight codes (two dwords) as f16.
-OSP_DEV f16x8 frag8(uint32_t a, uint32_t b) {
-  return frag(codes_f16(a, false), codes_f16(a, true), codes_f16(b, false), codes_f16(b, true));
-}
-OSP_DEV f32x4 mfma(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
 template <bool STREAM>
 OSP_DEV uint4 load16(const uint8_t* p) {
@@ -67,104 +48,16 @@ template <int HD> struct Page {
 #pragma unroll
     for (int i = 0; i < HD / 64; ++i) v[i] = load16<STREAM>(vp + 16 * i);
   }
-  OSP_DEV uint32_t kd(int i) const { return reinterpret_cast<const uint32_t*>(k)[i]; }
-  OSP_DEV uint32_t vd(int i) const { return reinterpret_cast<const uint32_t*>(v)[i]; }
+  OSP_DEV uint32_t kd(int i) const { return word(k, i); }
+  OSP_DEV uint32_t vd(int i) const { return word(v, i); }
 };
 
-// What a block works on.
-struct Item {
-  Kv8Seq s;
-  int b, tile, split, ns;
-};
-
-// Rows of sequence b and what they can see: no more than its table holds.
-OSP_DEV Kv8Seq attn_seq(const Kv8AttnArgs& a, int b) {
-  Kv8Seq s = kv8_seq(a.r, b);
-  s.ctx = min(s.ctx, a.pool.max_pages * kKv8Page);
-  return s;
-}
-
-// Splits of a pass.  split_len: the caller's, or an even deal of the tiles' positions over the
-// items that the launch aims at, no finer than the quantum and no more than n_split a sequence.
-OSP_DEV int plan_len(const Kv8AttnArgs& a, int cols, int group, int quantum, int lane) {
-  if (a.split_len > 0) return a.split_len;
-  float work = 0.f;
-  int longest = 1;
-  for (int b0 = 0; b0 < a.r.B; b0 += 64) {
-    const int b = b0 + lane;
-    if (b < a.r.B) {
-      const Kv8Seq s = attn_seq(a, b);
-      work += (float)(((s.end - s.beg) * group + cols - 1) / cols) * (float)s.ctx;
-      longest = max(longest, s.ctx);
-    }
-  }
-  if (a.r.B > 1) {
-    work = wave_sum(work);
-    longest = wave_max_i(longest);
-  } else {
-    work = lane_f(work, 0);
-    longest = lane_i(longest, 0);
-  }
-  const float even = work / (float)a.items;
-  int len = even < 1.0e9f ? (int)even + 1 : 1000000000;
-  len = max(len, (longest + a.n_split - 1) / a.n_split);
-  return (len + quantum - 1) / quantum * quantum;
-}
-
-// Item `it` of the pass: sequences in order, their tiles last to first (the last rows of a prompt
-// see most), a tile's splits in order.  False: there are fewer.
-OSP_DEV bool find_item(const Kv8AttnArgs& a, int it, int len, int cols, int group, int lane, Item& x) {
-  int before = 0;
-  for (int b0 = 0; b0 < a.r.B; b0 += 64) {
-    const int b = b0 + lane;
-    int tiles = 0, ns = 0;
-    if (b < a.r.B) {
-      const Kv8Seq s = attn_seq(a, b);
-      tiles = ((s.end - s.beg) * group + cols - 1) / cols;
-      ns = (s.ctx + len - 1) / len;
-    }
-    const int n = tiles * ns;
-    const int incl = a.r.B > 1 ? wave_incl_scan<int>(n) : n;
-    const uint64_t past = __builtin_amdgcn_ballot_w64(b < a.r.B && before + incl > it);
-    if (past) {
-      const int l = __builtin_ctzll(past);
-      x.b = b0 + l;
-      x.ns = lane_i(ns, l);
-      const int at = it - before - (lane_i(incl, l) - lane_i(n, l));
-      x.tile = lane_i(tiles, l) - 1 - at / x.ns;
-      x.split = at % x.ns;
-      x.s = attn_seq(a, x.b);
-      return true;
-    }
-    before += lane_i(incl, 63);
-    if (a.r.B <= 64) break;
-  }
-  return false;
-}
-
-// What a row sees: the positions before `lim`; with a tree those before `base` (the sequence's
-// first new position) and base + i for the set bits i of w.
-struct Sight {
-  int lim;
-  uint64_t w0, w1;
-};
-// Bit i: the row sees position t0 + i (i < 32).
-OSP_DEV uint32_t sight32(const Sight& s, bool tree, int base, int t0) {
-  const int n = s.lim - t0;
-  uint32_t v = n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u;
-  if (tree) {
-    const int r = t0 - base;
-    if (r >= 128) v = 0u;
-    else if (r >= 64) v &= (uint32_t)(s.w1 >> (r - 64));
-    else if (r > 32) v &= (uint32_t)(s.w0 >> r | s.w1 << (64 - r));
-    else if (r >= 0) v &= (uint32_t)(s.w0 >> r);
-    else if (r > -32) v &= (uint32_t)s.w0 << -r | ((1u << -r) - 1u);
-  }
-  return v;
-}
-
+constexpr int NP_(bool f) { return f ? 2 : 1; }
 template <int HD, int NT, bool F32, bool STREAM>
-__global__ void __launch_bounds__(256) k_kv8_attn(Kv8AttnArgs a) {
+#ifndef A_OCC
+#define A_OCC 2
+#endif
+__global__ void __launch_bounds__(256, (NT * NP_(F32) <= 2 ? A_OCC : 1)) k_kv8_attn(Kv8AttnArgs a) {
   constexpr int KC = HD / 32;         // K steps of the score product
   constexpr int DT = HD / 16;         // 16-row tiles of dims
   constexpr int NP = F32 ? 2 : 1;     // parts of Q and P
@@ -184,7 +77,7 @@ __global__ void __launch_bounds__(256) k_kv8_attn(Kv8AttnArgs a) {
     // ---- queries and what they see --------------------------------------------------
     f16x8 qf[NT][NP][KC];
     float colc[NT], m[NT], l[NT];
-    Sight see[NT];
+    int lim[NT];
     int lim_lo = 0x7fffffff, lim_hi = 0;
     bool missing = false;   // a visible position has no page
 #pragma unroll
@@ -207,9 +100,7 @@ __global__ void __launch_bounds__(256) k_kv8_attn(Kv8AttnArgs a) {
       for (int i = 0; i < HD / 4; ++i) big = fmaxf(big, fabsf(q[i]));
       big = fmaxf(big, xor_lane_c(big, 16));
       big = fmaxf(big, xor_lane_c(big, 32));
-      // 2^up takes the vector's largest magnitude into [2^13, 2^14)
-      const int e = (int)((__float_as_uint(big) >> 23) & 255) - 127;
-      const int up = big > 0.f && big < INFINITY ? min(max(13 - e, -114), 120) : 0;
+      const int up = query_exp(big);   // (largest magnitude into [2^13, 2^14))
       const float f = kv8_pow2(up);
       colc[nt] = kv8_pow2(-up) * (a.scale * kLog2e);
 #pragma unroll
@@ -224,20 +115,9 @@ __global__ void __launch_bounds__(256) k_kv8_attn(Kv8AttnArgs a) {
         qf[nt][0][c8] = hi;
         if constexpr (F32) qf[nt][NP - 1][c8] = lo;
       }
-      see[nt].lim = 0;
-      see[nt].w0 = see[nt].w1 = 0;
-      if (on) {
-        see[nt].lim = a.r.cached ? x.s.first + row - x.s.beg + 1 : max(a.r.pos[row], 0) + 1;
-        if (a.tree) {
-          see[nt].lim = x.s.ctx;
-          see[nt].w0 = a.tree[2 * (long)row];
-          see[nt].w1 = a.tree[2 * (long)row + 1];
-        }
-        missing |= see[nt].lim > x.s.ctx;
-        see[nt].lim = min(see[nt].lim, x.s.ctx);
-        lim_lo = min(lim_lo, a.tree ? min(x.s.first, x.s.ctx) : see[nt].lim);
-        lim_hi = max(lim_hi, see[nt].lim);
-      }
+      Sight see;
+      sight_of(a, x, row, on, see, lim_lo, lim_hi, missing);
+      lim[nt] = see.lim;
       m[nt] = kNoMax;
       l[nt] = 0.f;
     }
@@ -275,7 +155,7 @@ __global__ void __launch_bounds__(256) k_kv8_attn(Kv8AttnArgs a) {
       }
       const int ok = id >= 0 && has;
       id = max(id, 0);
-      // values relative to the largest scale: P times it stays within f16
+      // values are converted relative to the largest scale so far
       const float top = fmaxf(eref, wave_max(fabsf(sv)));
       if (top > eref) {
         if (eref > 0.f) {
@@ -303,81 +183,82 @@ __global__ void __launch_bounds__(256) k_kv8_attn(Kv8AttnArgs a) {
         const float rva = lane_f(rel, 2 * i), rvb = lane_f(rel, 2 * i + 1);
         const bool oka = lane_i(ok, 2 * i) != 0, okb = lane_i(ok, 2 * i + 1) != 0;
         const bool whole = t0 + 32 <= min(lim_lo, p_hi) && oka && okb;
-        f16x8 kf[2][KC];
+        f32x4 sc[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) sc[nt][0] = sc[nt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < 2; ++k)
 #pragma unroll
-          for (int c = 0; c < KC; ++c) kf[k][c] = frag8(pg[k].kd(2 * c), pg[k].kd(2 * c + 1));
-        if (!whole) {
-          // value codes past the context may be anything: 0 * NaN
+          for (int c = 0; c < KC; ++c) {
+            const f16x8 kf = frag8(pg[k].kd(2 * c), pg[k].kd(2 * c + 1));
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            const int left = (k ? okb : oka) ? x.s.ctx - (t0 + 16 * k + 4 * qr) : 0;
-            const uint32_t keep = left >= 4 ? 0xffffffffu : left <= 0 ? 0u : (1u << 8 * left) - 1u;
+            for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int d = 0; d < HD / 64; ++d) {
-              pg[k].v[d].x &= keep;
-              pg[k].v[d].y &= keep;
-              pg[k].v[d].z &= keep;
-              pg[k].v[d].w &= keep;
+              for (int p = 0; p < NP; ++p) sc[nt][k] = mfma(kf, qf[nt][p][c], sc[nt][k]);
+          }
+        float z[NT][8], top = -INFINITY;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+          exponents(sc[nt], score_factor(ska, colc[nt]), score_factor(skb, colc[nt]), kLift - m[nt], z[nt], top);
+        // One branch for all that is rare: pairs that some vector sees in part, maxima that move.
+        if (!whole || __builtin_amdgcn_ballot_w64(top > kLift + kSlack)) {
+          if (!whole) {
+            // value codes past the context may be anything: 0 * NaN
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              const int left = (k ? okb : oka) ? x.s.ctx - (t0 + 16 * k + 4 * qr) : 0;
+              const uint32_t keep = left >= 4 ? 0xffffffffu : left <= 0 ? 0u : (1u << 8 * left) - 1u;
+#pragma unroll
+              for (int d = 0; d < HD / 64; ++d) {
+                uint4& v = pg[k].v[d];
+                v = make_uint4(v.x & keep, v.y & keep, v.z & keep, v.w & keep);
+              }
             }
+          }
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            if (!whole) {
+              const uint32_t v = sight_now(a, x, c0 + 16 * nt + n16, group, lim[nt], t0) & in_pair(p_hi - t0, oka, okb);
+              mask_scores(sc[nt][0], v, qr);
+              mask_scores(sc[nt][1], v >> 16, qr);
+            }
+            const float fa = score_factor(ska, colc[nt]), fb = score_factor(skb, colc[nt]);
+            float cm = fmaxf(max4(sc[nt][0]) * fa, max4(sc[nt][1]) * fb);
+            cm = fmaxf(cm, xor_lane_c(cm, 16));
+            cm = fmaxf(cm, xor_lane_c(cm, 32));
+            const float mn = cm > m[nt] + kSlack ? ceilf(cm) : m[nt];
+            const float w = exp2f(m[nt] - mn);
+            m[nt] = mn;
+            l[nt] *= w;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) acc[nt][d] *= w;
+            exponents(sc[nt], fa, fb, kLift - m[nt], z[nt], top);
           }
         }
         f16x8 pf[NT][NP];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-          f32x4 s[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
-#pragma unroll
-          for (int k = 0; k < 2; ++k)
-#pragma unroll
-            for (int c = 0; c < KC; ++c)
-#pragma unroll
-              for (int p = 0; p < NP; ++p) s[k] = mfma(kf[k][c], qf[nt][p][c], s[k]);
-          const float fa = ska * colc[nt], fb = skb * colc[nt];
-          float y[8];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            y[e] = s[0][e] * fa;
-            y[4 + e] = s[1][e] * fb;
-          }
-          if (!whole) {
-            const int end = p_hi - t0;
-            const uint32_t in = (end >= 32 ? 0xffffffffu : (1u << end) - 1u) & (oka ? 0xffffffffu : 0xffff0000u) & (okb ? 0xffffffffu : 0xffffu);
-            const uint32_t sight = (sight32(see[nt], a.tree != nullptr, x.s.first, t0) & in) >> (4 * qr);
+          if constexpr (F32) {
+            f16x8 hi, lo;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-              if (!(sight >> ((e >> 2) * 16 + (e & 3)) & 1)) y[e] = -INFINITY;
+              const float p = __builtin_amdgcn_exp2f(z[nt][e]);
+              l[nt] += p;
+              hi[e] = (_Float16)p;
+              lo[e] = (_Float16)(p - (float)hi[e]);
             }
+            pf[nt][0] = hi;
+            pf[nt][NP - 1] = lo;
+          } else {
+            uint32_t u[4];
+            probabilities(z[nt], l[nt], u);
+            probabilities(z[nt] + 4, l[nt], u + 2);
+            pf[nt][0] = frag(u[0], u[1], u[2], u[3]);
           }
-          const float mx = fmaxf(fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])), fmaxf(fmaxf(y[4], y[5]), fmaxf(y[6], y[7])));
-          if (__builtin_amdgcn_ballot_w64(mx > m[nt] + kSlack)) {
-            float cm = fmaxf(mx, xor_lane_c(mx, 16));
-            cm = fmaxf(cm, xor_lane_c(cm, 32));
-            const float mn = fmaxf(m[nt], cm);
-            const float f = exp2f(m[nt] - mn);
-            m[nt] = mn;
-            l[nt] *= f;
-#pragma unroll
-            for (int d = 0; d < DT; ++d) acc[nt][d] *= f;
-          }
-          const float off = kLift - m[nt];
-          float p[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(y[e] + off);
-          l[nt] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
-          f16x8 hi, lo;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float w = p[e] * (e < 4 ? rva : rvb);
-            hi[e] = (_Float16)w;
-            if constexpr (F32) lo[e] = (_Float16)(w - (float)hi[e]);
-          }
-          pf[nt][0] = hi;
-          if constexpr (F32) pf[nt][NP - 1] = lo;
         }
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
-          const f16x8 vf = frag8(pg[0].vd(d), pg[1].vd(d));
+          const f16x8 vf = frag8(pg[0].vd(d), pg[1].vd(d), rva, rvb);
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -459,29 +340,52 @@ __global__ void __launch_bounds__(256) k_kv8_attn(Kv8AttnArgs a) {
   }
 }
 
-// One wavefront per (row, head): the splits' outputs, each with weight 2^(m_s - M).
-template <int HD>
+// The splits' outputs, each with weight 2^(m_s - M).  W wavefronts per (row, head) take the splits in
+// turn, every one of theirs requested at once: a join is two dependent loads long.
+template <int HD, int W>
 __global__ void __launch_bounds__(256) k_kv8_join(Kv8AttnArgs a) {
-  constexpr int E = HD / 64;
-  const int lane = threadIdx.x & 63;
-  const int w = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
-  const int row = w / a.nq, h = w % a.nq;
+  constexpr int E = HD / 64, PER = kKv8MaxSplits / W, G = 4 / W;   // G (row, head) pairs a block
+  __shared__ float sm[4][HD];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int i = blockIdx.x * G + wave / W, part = wave % W;
+  const int row = i / a.nq, h = i % a.nq;
   const int total = a.r.count ? min(*a.r.count, a.r.rows) : a.r.rows;
-  if (row >= total || (a.r.cu && row >= a.r.cu[a.r.B])) return;
-  const int ns = min(a.row_ns[row], a.n_split);
-  if (ns <= 1) return;   // (written by the attention itself)
-  const float* pp = a.part + ((long)row * a.nq + h) * a.n_split * (HD + 2);
-  const float m = lane < ns ? pp[(long)lane * (HD + 2)] : kNoMax;
-  const float ls = lane < ns ? pp[(long)lane * (HD + 2) + 1] : 0.f;
-  const float M = wave_max(m);
-  const float f = exp2f(m - M);
-  const float L = wave_sum(ls * f);
-  float o[E] = {};
-  for (int s = 0; s < ns; ++s) {
-    const float ws = lane_f(f, s);
+  const bool on = row < total && !(a.r.cu && row >= a.r.cu[a.r.B]);
+  const int ns = on ? min(a.row_ns[row], a.n_split) : 0;
+  float o[E] = {}, L = 0.f;
+  if (ns > 1) {   // (else written by the attention itself)
+    const float* pp = a.part + ((long)row * a.nq + h) * a.n_split * (HD + 2);
+    float v[PER][E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) o[e] += ws * pp[(long)s * (HD + 2) + 2 + lane * E + e];
+    for (int k = 0; k < PER; ++k)
+      if (part + k * W < ns) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[k][e] = pp[(long)(part + k * W) * (HD + 2) + 2 + lane * E + e];
+      }
+    const float m = lane < ns ? pp[(long)lane * (HD + 2)] : kNoMax;
+    const float ls = lane < ns ? pp[(long)lane * (HD + 2) + 1] : 0.f;
+    const float M = wave_max(m);
+    const float f = exp2f(m - M);
+    L = wave_sum(ls * f);
+#pragma unroll
+    for (int k = 0; k < PER; ++k)
+      if (part + k * W < ns) {
+        const float w = lane_f(f, part + k * W);
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] += w * v[k][e];
+      }
   }
+  if constexpr (W > 1) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) sm[wave][lane * E + e] = o[e];
+    __syncthreads();
+    if (part > 0) return;
+#pragma unroll
+    for (int w = 1; w < W; ++w)
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] += sm[wave + w][lane * E + e];
+  }
+  if (ns <= 1) return;
   const float inv = L > 0.f || L != L ? 1.f / L : 0.f;
   const long at = (long)row * a.ldo + (long)h * HD + lane * E;
 #pragma unroll
@@ -507,12 +411,14 @@ int cols_nt(int group, int max_rows) {
   const long c = (long)group * max_rows;
   return c <= 16 ? 1 : c <= 32 ? 2 : 4;
 }
+// Sequences of more query vectors than the widest tile here go to kv8_prompt.hip (bf16 rows: fp32
+// ones need twice the registers for their queries).
+bool use_prompt(const Kv8AttnArgs& a, int max_rows) { return a.x_bf16 && (long)(a.nq / a.pool.nkv) * max_rows > 64; }
 
 }  // namespace
 
-int kv8_attention_tiles(int rows, int B, int group, int max_rows) {
-  const int cols = 16 * cols_nt(group, max_rows);
-  return (int)((long)rows * group / cols) + B;
+int kv8_attention_cols(int x_bf16, int group, int max_rows) {
+  return x_bf16 && (long)group * max_rows > 64 ? kKv8PromptCols : 16 * cols_nt(group, max_rows);
 }
 
 void launch_kv8_attention(const Kv8AttnArgs& a, int max_rows, hipStream_t st) {
@@ -520,6 +426,7 @@ void launch_kv8_attention(const Kv8AttnArgs& a, int max_rows, hipStream_t st) {
   long y = (long)a.tiles * a.n_split;
   if (a.split_len == 0 && a.n_split > 1) y = std::min<long>(y, (long)a.items + a.tiles);
   const dim3 grid(a.pool.nkv, (unsigned)std::min<long>(std::max<long>(y, 1), 65535));
+  if (use_prompt(a, max_rows)) return launch_kv8_prompt(a, grid, st);
   if (a.hd == 128) {
     if (nt == 1) launch_cols<128, 1>(a, grid, st);
     else if (nt == 2) launch_cols<128, 2>(a, grid, st);
@@ -532,9 +439,17 @@ void launch_kv8_attention(const Kv8AttnArgs& a, int max_rows, hipStream_t st) {
 }
 
 void launch_kv8_join(const Kv8AttnArgs& a, hipStream_t st) {
-  const dim3 grid((unsigned)(((long)a.r.rows * a.nq + 3) / 4));
-  if (a.hd == 128) hipLaunchKernelGGL(k_kv8_join<128>, grid, dim3(256), 0, st, a);
-  else hipLaunchKernelGGL(k_kv8_join<64>, grid, dim3(256), 0, st, a);
+  // few outputs: the latency of a wavefront's loads is the time; many: fewer wavefronts read more each
+  const long n = (long)a.r.rows * a.nq;
+  if (n <= 1024) {
+    const dim3 grid((unsigned)n);
+    if (a.hd == 128) hipLaunchKernelGGL((k_kv8_join<128, 4>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((k_kv8_join<64, 4>), grid, dim3(256), 0, st, a);
+  } else {
+    const dim3 grid((unsigned)((n + 3) / 4));
+    if (a.hd == 128) hipLaunchKernelGGL((k_kv8_join<128, 1>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((k_kv8_join<64, 1>), grid, dim3(256), 0, st, a);
+  }
 }
 
 }  // namespace osp

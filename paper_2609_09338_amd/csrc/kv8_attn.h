@@ -1,0 +1,223 @@
+// Device code that the attention kernels over the 8-bit cache share: conversions, the deal of
+// the work, what a row sees.
+#pragma once
+
+#include "kv8.h"
+
+namespace osp {
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kNoMax = -1.0e30f;   // below any score: a row that has seen nothing
+constexpr float kLift = 6.f;         // P's largest value is 2^kLift, 2^(kLift + kSlack) before the maximum moves
+constexpr float kSlack = 8.f;
+
+OSP_DEV uint32_t h2(f16x2 v) { return __builtin_bit_cast(uint32_t, v); }
+// Two of a dword's codes as f16, times a power of two.
+OSP_DEV uint32_t codes_f16(uint32_t u, bool hi, float r) {
+  return hi ? h2(__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(u, r, true)) : h2(__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(u, r, false));
+}
+OSP_DEV f16x8 frag(uint32_t a, uint32_t b, uint32_t c, uint32_t d) { return __builtin_bit_cast(f16x8, make_uint4(a, b, c, d)); }
+// Dword i of a lane's 16-byte pieces (i a constant once loops are unrolled: the pieces stay in registers).
+OSP_DEV uint32_t word(const uint4* r, int i) {
+  const uint4& v = r[i >> 2];
+  switch (i & 3) {
+    case 0: return v.x;
+    case 1: return v.y;
+    case 2: return v.z;
+    default: return v.w;
+  }
+}
+// Eight codes (two dwords) as f16, times ra and rb.
+OSP_DEV f16x8 frag8(uint32_t a, uint32_t b, float ra = 1.f, float rb = 1.f) {
+  return frag(codes_f16(a, false, ra), codes_f16(a, true, ra), codes_f16(b, false, rb), codes_f16(b, true, rb));
+}
+OSP_DEV f32x4 mfma(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+
+// What a block works on.
+struct Item {
+  Kv8Seq s;
+  int b, tile, split, ns;
+};
+
+// Rows of sequence b and what they can see: no more than its table holds.
+OSP_DEV Kv8Seq attn_seq(const Kv8AttnArgs& a, int b) {
+  Kv8Seq s = kv8_seq(a.r, b);
+  s.ctx = min(s.ctx, a.pool.max_pages * kKv8Page);
+  return s;
+}
+
+// Splits of a pass.  split_len: the caller's, or an even deal of the tiles' positions over the
+// items that the launch aims at, no finer than the quantum and no more than n_split a sequence.
+OSP_DEV int plan_len(const Kv8AttnArgs& a, int cols, int group, int quantum, int lane) {
+  if (a.split_len > 0) return a.split_len;
+  float work = 0.f;
+  int longest = 1;
+  for (int b0 = 0; b0 < a.r.B; b0 += 64) {
+    const int b = b0 + lane;
+    if (b < a.r.B) {
+      const Kv8Seq s = attn_seq(a, b);
+      work += (float)(((s.end - s.beg) * group + cols - 1) / cols) * (float)s.ctx;
+      longest = max(longest, s.ctx);
+    }
+  }
+  if (a.r.B > 1) {
+    work = wave_sum(work);
+    longest = wave_max_i(longest);
+  } else {
+    work = lane_f(work, 0);
+    longest = lane_i(longest, 0);
+  }
+  const float even = work / (float)a.items;
+  int len = even < 1.0e9f ? (int)even + 1 : 1000000000;
+  len = max(len, (longest + a.n_split - 1) / a.n_split);
+  return (len + quantum - 1) / quantum * quantum;
+}
+
+// Item `it` of the pass: sequences in order, their tiles last to first (the last rows of a prompt
+// see most), a tile's splits in order.  False: there are fewer.
+OSP_DEV bool find_item(const Kv8AttnArgs& a, int it, int len, int cols, int group, int lane, Item& x) {
+  int before = 0;
+  for (int b0 = 0; b0 < a.r.B; b0 += 64) {
+    const int b = b0 + lane;
+    int tiles = 0, ns = 0;
+    if (b < a.r.B) {
+      const Kv8Seq s = attn_seq(a, b);
+      tiles = ((s.end - s.beg) * group + cols - 1) / cols;
+      ns = (s.ctx + len - 1) / len;
+    }
+    const int n = tiles * ns;
+    const int incl = a.r.B > 1 ? wave_incl_scan<int>(n) : n;
+    const uint64_t past = __builtin_amdgcn_ballot_w64(b < a.r.B && before + incl > it);
+    if (past) {
+      const int l = __builtin_ctzll(past);
+      x.b = b0 + l;
+      x.ns = lane_i(ns, l);
+      const int at = it - before - (lane_i(incl, l) - lane_i(n, l));
+      x.tile = lane_i(tiles, l) - 1 - at / x.ns;
+      x.split = at % x.ns;
+      x.s = attn_seq(a, x.b);
+      return true;
+    }
+    before += lane_i(incl, 63);
+    if (a.r.B <= 64) break;
+  }
+  return false;
+}
+
+// What a row sees: the positions before `lim`; with a tree those before `base` (the sequence's
+// first new position) and base + i for the set bits i of w.
+struct Sight {
+  int lim;
+  uint64_t w0, w1;
+};
+// Bit i: the row sees position t0 + i (i < 32).
+OSP_DEV uint32_t sight32(const Sight& s, bool tree, int base, int t0) {
+  const int n = s.lim - t0;
+  uint32_t v = n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u;
+  if (tree) {
+    const int r = t0 - base;
+    if (r >= 128) v = 0u;
+    else if (r >= 64) v &= (uint32_t)(s.w1 >> (r - 64));
+    else if (r > 32) v &= (uint32_t)(s.w0 >> r | s.w1 << (64 - r));
+    else if (r >= 0) v &= (uint32_t)(s.w0 >> r);
+    else if (r > -32) v &= (uint32_t)s.w0 << -r | ((1u << -r) - 1u);
+  }
+  return v;
+}
+
+// A row's place in the pass: what it sees, the tile's shortest and longest view, and whether
+// some of it lies past the table.
+OSP_DEV void sight_of(const Kv8AttnArgs& a, const Item& x, int row, bool on, Sight& s, int& lo, int& hi, bool& missing) {
+  s.lim = 0;
+  s.w0 = s.w1 = 0;
+  if (!on) return;
+  s.lim = a.r.cached ? x.s.first + row - x.s.beg + 1 : max(a.r.pos[row], 0) + 1;
+  if (a.tree) {
+    s.lim = x.s.ctx;
+    s.w0 = a.tree[2 * (long)row];
+    s.w1 = a.tree[2 * (long)row + 1];
+  }
+  missing |= s.lim > x.s.ctx;
+  s.lim = min(s.lim, x.s.ctx);
+  lo = min(lo, a.tree ? min(x.s.first, x.s.ctx) : s.lim);
+  hi = max(hi, s.lim);
+}
+
+// sight32 of vector c of the item's sequence, its tree words read now: few tokens need them.
+OSP_DEV uint32_t sight_now(const Kv8AttnArgs& a, const Item& x, int c, int group, int lim, int t0) {
+  Sight s{lim, 0, 0};
+  if (a.tree && lim > 0 && t0 + 32 > x.s.first) {
+    const long row = x.s.beg + c / group;
+    s.w0 = a.tree[2 * row];
+    s.w1 = a.tree[2 * row + 1];
+  }
+  return sight32(s, a.tree != nullptr, x.s.first, t0);
+}
+
+// The tokens of a pair (bit i: the i-th) that lie in the split (`end`: its positions from the
+// pair's first one on) and on a page.
+OSP_DEV uint32_t in_pair(int end, bool oka, bool okb) {
+  return (end >= 32 ? 0xffffffffu : end <= 0 ? 0u : (1u << end) - 1u) & (oka ? 0xffffffffu : 0xffff0000u) & (okb ? 0xffffffffu : 0xffffu);
+}
+// The lane's four scores of a page's tokens 4 qr + e: -inf where bit 4 qr + e of `sight` is clear.
+OSP_DEV void mask_scores(f32x4& s, uint32_t sight, int qr) {
+  const uint32_t v = sight >> (4 * qr);
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (!(v >> e & 1)) s[e] = -INFINITY;
+}
+// The factor of a page's scores: never zero, so that a masked one stays -inf.
+OSP_DEV float score_factor(float sk, float colc) { return fmaxf(sk * colc, 1.2e-38f); }
+OSP_DEV float max4(f32x4 s) { return fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])); }
+
+// The power of two that takes a query vector's largest magnitude into [2^13, 2^14).
+OSP_DEV int query_exp(float big) {
+  const int e = (int)((__float_as_uint(big) >> 23) & 255) - 127;
+  return big > 0.f && big < INFINITY ? min(max(13 - e, -114), 120) : 0;
+}
+
+// The lane's HD / 4 dims of a bf16 query vector as B operands (exact); the factor of its scores.
+template <int HD>
+OSP_DEV float query_frags(const bf16_t* p, float scale, f16x8* qf) {
+  float q[HD / 4], big = 0.f;
+#pragma unroll
+  for (int i = 0; i < HD / 4; i += 8) load_vec<bf16_t>(p + i, q + i);
+#pragma unroll
+  for (int i = 0; i < HD / 4; ++i) big = fmaxf(big, fabsf(q[i]));
+  big = fmaxf(big, xor_lane_c(big, 16));
+  big = fmaxf(big, xor_lane_c(big, 32));
+  const int up = query_exp(big);
+  const float f = kv8_pow2(up);
+#pragma unroll
+  for (int c = 0; c < HD / 32; ++c)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) qf[c][j] = (_Float16)(q[c * 8 + j] * f);
+  return kv8_pow2(-up) * (scale * kLog2e);
+}
+
+// P = 2^z of a lane's four exponents as f16; its sum (of the rounded values) joins l.
+OSP_DEV void probabilities(const float* z, float& l, uint32_t* u) {
+  const f16x2 one = {(_Float16)1.f, (_Float16)1.f};
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const f16x2 h = {(_Float16)__builtin_amdgcn_exp2f(z[2 * e]), (_Float16)__builtin_amdgcn_exp2f(z[2 * e + 1])};
+    l = __builtin_amdgcn_fdot2(h, one, l, false);
+    u[e] = h2(h);
+  }
+}
+// z = s f + up of a pair's eight scores; their maximum joins top.
+OSP_DEV void exponents(const f32x4* s, float fa, float fb, float up, float* z, float& top) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    z[e] = __builtin_fmaf(s[e >> 2][e & 3], e < 4 ? fa : fb, up);
+    top = fmaxf(top, z[e]);
+  }
+}
+
+}  // namespace
+}  // namespace osp
