@@ -11,8 +11,9 @@
 //   O^T[dim][query] += V^T P^T    (16x16x32, the K index runs over 4 q .. 4 q + 3 of both pages)
 // where lane (l % 16, q = l / 16) of the score tile holds exactly the four tokens of each page that
 // the second product's B operand wants there: nothing moves between lanes in the loop.
-//   * Queries are scaled by a power of two per vector into f16's range: bf16 queries are then
-//     exact (f16 keeps 11 bits), fp32 ones go in as hi + lo (22 bits, two products).
+//   * bf16 queries go in as they are, beside codes converted to bf16 (exact).  fp32 queries are
+//     scaled by a power of two per vector into f16's range and go in as hi + lo (22 bits, two
+//     products) beside f16 codes.
 //   * A key block's scale and the softmax scale are one factor of the exponent's fma.  A value
 //     block's scale, relative to the largest of the wavefront's pages so far, is an operand of its
 //     codes' conversion.  P is held in f16 with 2^6 .. 2^14 as its largest value: 11 bits down to
@@ -22,6 +23,7 @@
 //     cross-lane traffic otherwise), and then to a whole number: outputs are rescaled by powers of
 //     two, exactly.  Sums stay per lane until the end.
 #include <algorithm>
+#include <type_traits>
 
 #include "kv8_attn.h"
 
@@ -61,21 +63,49 @@ __global__ void __launch_bounds__(256, (NT * NP_(F32) <= 2 ? A_OCC : 1)) k_kv8_a
   constexpr int KC = HD / 32;         // K steps of the score product
   constexpr int DT = HD / 16;         // 16-row tiles of dims
   constexpr int NP = F32 ? 2 : 1;     // parts of Q and P
+#ifndef A_DEPTH
+#define A_DEPTH 2
+#endif
+  constexpr int DEPTH = NT * NP == 1 ? A_DEPTH : 2;   // pairs in flight
   constexpr int COLS = 16 * NT;
-  __shared__ float sm_o[4][16][HD + 4];
+  __shared__ float sm_o[4][COLS][HD + 4];
   __shared__ float sm_m[4][COLS], sm_l[4][COLS];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = blockIdx.x, group = a.nq / a.pool.nkv;
   const int n16 = lane & 15, qr = lane >> 4;
-  const int len = plan_len(a, COLS, group, 128, lane);
+  const Deal deal = deal_of(a, COLS, group, 128, lane);
+  const int len = deal.len;
 
   for (int it = blockIdx.y;; it += gridDim.y) {
     Item x;
-    if (!find_item(a, it, len, COLS, group, lane, x)) return;
+    if (!find_item(a, deal, it, COLS, group, lane, x)) return;
     const int nvec = (x.s.end - x.s.beg) * group, c0 = x.tile * COLS;
 
+    // ---- the split's page pairs: wave, wave + 4, ... ---------------------------------
+    // Requested before anything else: the first pages, then the queries, then the scales.
+    const int p_lo = x.split * len, s_hi = min(p_lo + len, x.s.ctx);
+    const long k_off = (long)g * (kKv8Page * HD) + n16 * HD + qr * (HD / 4);
+    const long v_off = (long)(a.pool.nkv + g) * (kKv8Page * HD) + qr * 4 * HD + n16 * (HD / 4);
+    // 32 of the wavefront's pairs at a time, a page a lane (-1: none, -2: not in the split)
+    auto pages_at = [&](int i0) {
+      const int t = p_lo + (wave + 4 * (i0 + (lane >> 1))) * 32 + (lane & 1) * 16;
+      return t < s_hi ? kv8_page(a.pool, x.b, t / kKv8Page) : -2;
+    };
+    int id = pages_at(0);
+    Page<HD> buf[DEPTH][2];
+    auto request = [&](Page<HD>(&pg)[2], int i) {   // (past the last: any page of the pool, unused)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const uint8_t* base = a.pool.codes + (long)max(lane_i(id, min(2 * i + k, 63)), 0) * a.pool.page_stride;
+        pg[k].template load<STREAM>(base + k_off, base + v_off);
+      }
+    };
+#pragma unroll
+    for (int i = 0; i + 1 < DEPTH; ++i) request(buf[i], i);
+
     // ---- queries and what they see --------------------------------------------------
-    f16x8 qf[NT][NP][KC];
+    typedef typename std::conditional<F32, f16x8, bf16x8>::type qk_t;
+    qk_t qf[NT][NP][KC];
     float colc[NT], m[NT], l[NT];
     int lim[NT];
     int lim_lo = 0x7fffffff, lim_hi = 0;
@@ -85,35 +115,31 @@ __global__ void __launch_bounds__(256, (NT * NP_(F32) <= 2 ? A_OCC : 1)) k_kv8_a
       const int c = c0 + 16 * nt + n16;
       const bool on = c < nvec;
       const int row = x.s.beg + (on ? c / group : 0), h = g * group + (on ? c % group : 0);
-      float q[HD / 4];
-      if (F32) {
-        const float* p = reinterpret_cast<const float*>(a.q) + (long)row * a.ldq + (long)h * HD + qr * (HD / 4);
+      const long at = (long)row * a.ldq + (long)h * HD + qr * (HD / 4);
+      colc[nt] = a.scale * kLog2e;
+      if constexpr (F32) {
+        const float* p = reinterpret_cast<const float*>(a.q) + at;
+        float q[HD / 4], big = 0.f;
 #pragma unroll
         for (int i = 0; i < HD / 4; i += 4) load_vec<float>(p + i, q + i);
-      } else {
-        const bf16_t* p = reinterpret_cast<const bf16_t*>(a.q) + (long)row * a.ldq + (long)h * HD + qr * (HD / 4);
 #pragma unroll
-        for (int i = 0; i < HD / 4; i += 8) load_vec<bf16_t>(p + i, q + i);
-      }
-      float big = 0.f;
+        for (int i = 0; i < HD / 4; ++i) big = fmaxf(big, fabsf(q[i]));
+        big = fmaxf(big, xor_lane_c(big, 16));
+        big = fmaxf(big, xor_lane_c(big, 32));
+        const int up = query_exp(big);
+        const float f = kv8_pow2(up);
+        colc[nt] *= kv8_pow2(-up);
 #pragma unroll
-      for (int i = 0; i < HD / 4; ++i) big = fmaxf(big, fabsf(q[i]));
-      big = fmaxf(big, xor_lane_c(big, 16));
-      big = fmaxf(big, xor_lane_c(big, 32));
-      const int up = query_exp(big);   // (largest magnitude into [2^13, 2^14))
-      const float f = kv8_pow2(up);
-      colc[nt] = kv8_pow2(-up) * (a.scale * kLog2e);
-#pragma unroll
-      for (int c8 = 0; c8 < KC; ++c8) {
-        f16x8 hi, lo;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float v = q[c8 * 8 + j] * f;
-          hi[j] = (_Float16)v;
-          lo[j] = (_Float16)(v - (float)hi[j]);
+        for (int i = 0; i < HD / 4; ++i) {
+          const float v = q[i] * f;
+          const _Float16 hi = (_Float16)v;
+          qf[nt][0][i / 8][i % 8] = hi;
+          qf[nt][NP - 1][i / 8][i % 8] = (_Float16)(v - (float)hi);
         }
-        qf[nt][0][c8] = hi;
-        if constexpr (F32) qf[nt][NP - 1][c8] = lo;
+      } else {
+        const uint4* p = reinterpret_cast<const uint4*>(reinterpret_cast<const bf16_t*>(a.q) + at);
+#pragma unroll
+        for (int i = 0; i < KC; ++i) qf[nt][0][i] = __builtin_bit_cast(bf16x8, p[i]);
       }
       Sight see;
       sight_of(a, x, row, on, see, lim_lo, lim_hi, missing);
@@ -130,31 +156,25 @@ __global__ void __launch_bounds__(256, (NT * NP_(F32) <= 2 ? A_OCC : 1)) k_kv8_a
 #pragma unroll
       for (int d = 0; d < DT; ++d) acc[nt][d] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    // ---- the split's page pairs: wave, wave + 4, ... ---------------------------------
-    const int p_lo = x.split * len, p_hi = min(p_lo + len, lim_hi);
+    const int p_hi = min(s_hi, lim_hi);
     const int n_pairs = p_hi > p_lo ? (p_hi - p_lo + 31) / 32 : 0;
     const int mine = n_pairs > wave ? (n_pairs - wave + 3) / 4 : 0;
-    const long k_off = (long)g * (kKv8Page * HD) + lane % 16 * HD + qr * (HD / 4);
-    const long v_off = (long)(a.pool.nkv + g) * (kKv8Page * HD) + qr * 4 * HD + n16 * (HD / 4);
     float eref = 0.f;     // largest value scale so far (0: none)
-    // 32 pairs at a time: a page and its scales a lane
     for (int i0 = 0; i0 < mine; i0 += 32) {
       const int todo = min(32, mine - i0);
-      const int t_lane = p_lo + (wave + 4 * (i0 + (lane >> 1))) * 32 + (lane & 1) * 16;
-      int id = 0;
-      float sk = 0.f, sv = 0.f;
-      const bool has = (lane >> 1) < todo && t_lane < p_hi;
-      if (has) {
-        id = kv8_page(a.pool, x.b, t_lane / kKv8Page);
-        missing |= id < 0;
-        if (id >= 0) {
-          const float* s = a.pool.scales + (long)id * a.pool.scale_stride + 2 * g;
-          sk = s[0];
-          sv = s[1];
-        }
+      if (i0 > 0) {
+        id = pages_at(i0);
+#pragma unroll
+        for (int i = 0; i + 1 < DEPTH; ++i) request(buf[i], i);
       }
-      const int ok = id >= 0 && has;
-      id = max(id, 0);
+      float sk = 0.f, sv = 0.f;
+      if (id >= 0) {
+        const float* s = a.pool.scales + (long)id * a.pool.scale_stride + 2 * g;
+        sk = s[0];
+        sv = s[1];
+      }
+      missing |= id == -1;
+      const int ok = id >= 0;
       // values are converted relative to the largest scale so far
       const float top = fmaxf(eref, wave_max(fabsf(sv)));
       if (top > eref) {
@@ -169,14 +189,6 @@ __global__ void __launch_bounds__(256, (NT * NP_(F32) <= 2 ? A_OCC : 1)) k_kv8_a
       }
       const float rel = eref > 0.f ? sv / eref : 0.f;
 
-      Page<HD> buf[2][2];
-      auto request = [&](Page<HD>(&pg)[2], int i) {
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const uint8_t* base = a.pool.codes + (long)lane_i(id, min(2 * i + k, 63)) * a.pool.page_stride;
-          pg[k].template load<STREAM>(base + k_off, base + v_off);
-        }
-      };
       auto step = [&](Page<HD>(&pg)[2], int i) {
         const int t0 = p_lo + (wave + 4 * (i0 + i)) * 32;
         const float ska = lane_f(sk, 2 * i), skb = lane_f(sk, 2 * i + 1);
@@ -190,7 +202,9 @@ __global__ void __launch_bounds__(256, (NT * NP_(F32) <= 2 ? A_OCC : 1)) k_kv8_a
         for (int k = 0; k < 2; ++k)
 #pragma unroll
           for (int c = 0; c < KC; ++c) {
-            const f16x8 kf = frag8(pg[k].kd(2 * c), pg[k].kd(2 * c + 1));
+            qk_t kf;
+            if constexpr (F32) kf = frag8(pg[k].kd(2 * c), pg[k].kd(2 * c + 1));
+            else kf = frag8_bf16(pg[k].kd(2 * c), pg[k].kd(2 * c + 1));
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -265,21 +279,20 @@ __global__ void __launch_bounds__(256, (NT * NP_(F32) <= 2 ? A_OCC : 1)) k_kv8_a
             for (int p = 0; p < NP; ++p) acc[nt][d] = mfma(vf, pf[nt][p], acc[nt][d]);
         }
       };
-      request(buf[0], 0);
-      for (int i = 0; i < todo; i += 2) {
-        request(buf[1], i + 1);   // (past the last: page 0 of the pool or the last one's neighbour, unused)
-        step(buf[0], i);
-        if (i + 1 < todo) {
-          request(buf[0], i + 2);
-          step(buf[1], i + 1);
-        }
+      // (a ring without copies: a copy would wait for its load)
+      for (int i = 0; i < todo; i += DEPTH) {
+#pragma unroll
+        for (int u = 0; u < DEPTH; ++u)
+          if (i + u < todo) {
+            request(buf[(u + DEPTH - 1) % DEPTH], i + u + DEPTH - 1);
+            step(buf[u], i + u);
+          }
       }
     }
     if (missing && a.err) atomicOr(a.err, 1u << 2);
 
     // ---- merge the wavefronts --------------------------------------------------------
     const bool direct = x.ns == 1 && a.out != nullptr;   // one split: no join
-    const float vs = eref > 0.f ? eref : 0.f;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       l[nt] += xor_lane_c(l[nt], 16);
@@ -288,51 +301,48 @@ __global__ void __launch_bounds__(256, (NT * NP_(F32) <= 2 ? A_OCC : 1)) k_kv8_a
         sm_m[wave][16 * nt + n16] = m[nt];
         sm_l[wave][16 * nt + n16] = l[nt];
       }
-    }
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      __syncthreads();   // (the tile before has been read)
 #pragma unroll
       for (int d = 0; d < DT; ++d)
-        *reinterpret_cast<float4*>(&sm_o[wave][n16][16 * d + 4 * qr]) =
-            make_float4(acc[nt][d][0] * vs, acc[nt][d][1] * vs, acc[nt][d][2] * vs, acc[nt][d][3] * vs);
-      __syncthreads();
-      for (int i = threadIdx.x; i < 16 * HD / 4; i += 256) {
-        const int j = i / (HD / 4), e = i % (HD / 4) * 4, c = c0 + 16 * nt + j;
-        if (c >= nvec) continue;
-        float M = kNoMax;
+        *reinterpret_cast<float4*>(&sm_o[wave][16 * nt + n16][16 * d + 4 * qr]) =
+            make_float4(acc[nt][d][0] * eref, acc[nt][d][1] * eref, acc[nt][d][2] * eref, acc[nt][d][3] * eref);
+    }
+    __syncthreads();
+#pragma unroll 1
+    for (int i = threadIdx.x; i < COLS * HD / 4; i += 256) {
+      const int j = i / (HD / 4), e = i % (HD / 4) * 4, c = c0 + j;
+      if (c >= nvec) break;   // (j ascends)
+      float M = kNoMax;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) M = fmaxf(M, sm_m[w][16 * nt + j]);
-        float L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+      for (int w = 0; w < 4; ++w) M = fmaxf(M, sm_m[w][j]);
+      float L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          const float f = exp2f(sm_m[w][16 * nt + j] - M);
-          L += sm_l[w][16 * nt + j] * f;
-          const float4 v = *reinterpret_cast<const float4*>(&sm_o[w][j][e]);
-          o[0] += v.x * f;
-          o[1] += v.y * f;
-          o[2] += v.z * f;
-          o[3] += v.w * f;
-        }
-        const int row = x.s.beg + c / group, h = g * group + c % group;
-        if (e == 0 && h == 0 && x.split == 0 && a.row_ns) a.row_ns[row] = x.ns;
-        if (direct) {
-          const float inv = L > 0.f || L != L ? 1.f / L : 0.f;
-          const long at = (long)row * a.ldo + (long)h * HD + e;
-          if (a.x_bf16)
-            *reinterpret_cast<uint2*>(reinterpret_cast<bf16_t*>(a.out) + at) =
-                make_uint2(f32x2_to_bf16x2(o[0] * inv, o[1] * inv), f32x2_to_bf16x2(o[2] * inv, o[3] * inv));
-          else
-            *reinterpret_cast<float4*>(reinterpret_cast<float*>(a.out) + at) = make_float4(o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
-        } else {
-          float* pp = a.part + (((long)row * a.nq + h) * a.n_split + x.split) * (HD + 2);
-          *reinterpret_cast<float2*>(pp + 2 + e) = make_float2(o[0], o[1]);
-          *reinterpret_cast<float2*>(pp + 4 + e) = make_float2(o[2], o[3]);
-          if (e == 0) {
-            // (P was lifted by 2^kLift)
-            pp[0] = a.natural ? (M > kNoMax ? (M - kLift) * kLn2 : -INFINITY) : M;
-            pp[1] = L;
-          }
+      for (int w = 0; w < 4; ++w) {
+        const float f = exp2f(sm_m[w][j] - M);
+        L += sm_l[w][j] * f;
+        const float4 v = *reinterpret_cast<const float4*>(&sm_o[w][j][e]);
+        o[0] += v.x * f;
+        o[1] += v.y * f;
+        o[2] += v.z * f;
+        o[3] += v.w * f;
+      }
+      const int row = x.s.beg + c / group, h = g * group + c % group;
+      if (e == 0 && h == 0 && x.split == 0 && a.row_ns) a.row_ns[row] = x.ns;
+      if (direct) {
+        const float inv = L > 0.f || L != L ? 1.f / L : 0.f;
+        const long at = (long)row * a.ldo + (long)h * HD + e;
+        if constexpr (F32)
+          *reinterpret_cast<float4*>(reinterpret_cast<float*>(a.out) + at) = make_float4(o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+        else
+          *reinterpret_cast<uint2*>(reinterpret_cast<bf16_t*>(a.out) + at) =
+              make_uint2(f32x2_to_bf16x2(o[0] * inv, o[1] * inv), f32x2_to_bf16x2(o[2] * inv, o[3] * inv));
+      } else {
+        float* pp = a.part + (((long)row * a.nq + h) * a.n_split + x.split) * (HD + 2);
+        *reinterpret_cast<float2*>(pp + 2 + e) = make_float2(o[0], o[1]);
+        *reinterpret_cast<float2*>(pp + 4 + e) = make_float2(o[2], o[3]);
+        if (e == 0) {
+          // (P was lifted by 2^kLift)
+          pp[0] = a.natural ? (M > kNoMax ? (M - kLift) * kLn2 : -INFINITY) : M;
+          pp[1] = L;
         }
       }
     }
@@ -344,7 +354,7 @@ __global__ void __launch_bounds__(256, (NT * NP_(F32) <= 2 ? A_OCC : 1)) k_kv8_a
 // turn, every one of theirs requested at once: a join is two dependent loads long.
 template <int HD, int W>
 __global__ void __launch_bounds__(256) k_kv8_join(Kv8AttnArgs a) {
-  constexpr int E = HD / 64, PER = kKv8MaxSplits / W, G = 4 / W;   // G (row, head) pairs a block
+  constexpr int E = HD / 64, PER = 16, G = 4 / W;   // G (row, head) pairs a block
   __shared__ float sm[4][HD];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int i = blockIdx.x * G + wave / W, part = wave % W;
@@ -355,25 +365,29 @@ __global__ void __launch_bounds__(256) k_kv8_join(Kv8AttnArgs a) {
   float o[E] = {}, L = 0.f;
   if (ns > 1) {   // (else written by the attention itself)
     const float* pp = a.part + ((long)row * a.nq + h) * a.n_split * (HD + 2);
-    float v[PER][E];
-#pragma unroll
-    for (int k = 0; k < PER; ++k)
-      if (part + k * W < ns) {
-#pragma unroll
-        for (int e = 0; e < E; ++e) v[k][e] = pp[(long)(part + k * W) * (HD + 2) + 2 + lane * E + e];
-      }
     const float m = lane < ns ? pp[(long)lane * (HD + 2)] : kNoMax;
     const float ls = lane < ns ? pp[(long)lane * (HD + 2) + 1] : 0.f;
-    const float M = wave_max(m);
-    const float f = exp2f(m - M);
-    L = wave_sum(ls * f);
+    float f = 0.f;
+    for (int s0 = 0; s0 < ns; s0 += PER * W) {
+      float v[PER][E];
 #pragma unroll
-    for (int k = 0; k < PER; ++k)
-      if (part + k * W < ns) {
-        const float w = lane_f(f, part + k * W);
+      for (int k = 0; k < PER; ++k) {
+        const long s = min(s0 + part + k * W, ns - 1);   // (past the last: read again, weight 0)
 #pragma unroll
-        for (int e = 0; e < E; ++e) o[e] += w * v[k][e];
+        for (int e = 0; e < E; ++e) v[k][e] = pp[s * (HD + 2) + 2 + lane * E + e];
       }
+      if (s0 == 0) {
+        f = exp2f(m - wave_max(m));
+        L = wave_sum(ls * f);
+      }
+#pragma unroll
+      for (int k = 0; k < PER; ++k) {
+        const int s = s0 + part + k * W;
+        const float w = s < ns ? lane_f(f, s) : 0.f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] += s < ns ? w * v[k][e] : 0.f;
+      }
+    }
   }
   if constexpr (W > 1) {
 #pragma unroll
@@ -406,35 +420,29 @@ void launch_cols(const Kv8AttnArgs& a, dim3 grid, hipStream_t st) {
   }
 }
 
-// 16-column tiles of a launch: enough for a sequence's query vectors, at most four.
-int cols_nt(int group, int max_rows) {
-  const long c = (long)group * max_rows;
-  return c <= 16 ? 1 : c <= 32 ? 2 : 4;
-}
-// Sequences of more query vectors than the widest tile here go to kv8_prompt.hip (bf16 rows: fp32
-// ones need twice the registers for their queries).
-bool use_prompt(const Kv8AttnArgs& a, int max_rows) { return a.x_bf16 && (long)(a.nq / a.pool.nkv) * max_rows > 64; }
+// Sequences of at most 32 query vectors a kv head, and fp32 rows (whose queries take twice the
+// registers), go to the kernel here; more to kv8_prompt.hip.
+bool use_prompt(int x_bf16, int group, int max_rows) { return x_bf16 && (long)group * max_rows > 32; }
+int cols_nt(int group, int max_rows) { return (long)group * max_rows <= 16 ? 1 : 2; }
 
 }  // namespace
 
 int kv8_attention_cols(int x_bf16, int group, int max_rows) {
-  return x_bf16 && (long)group * max_rows > 64 ? kKv8PromptCols : 16 * cols_nt(group, max_rows);
+  return use_prompt(x_bf16, group, max_rows) ? kKv8PromptCols : 16 * cols_nt(group, max_rows);
 }
 
 void launch_kv8_attention(const Kv8AttnArgs& a, int max_rows, hipStream_t st) {
-  const int nt = cols_nt(a.nq / a.pool.nkv, max_rows);
+  const int group = a.nq / a.pool.nkv, nt = cols_nt(group, max_rows);
   long y = (long)a.tiles * a.n_split;
   if (a.split_len == 0 && a.n_split > 1) y = std::min<long>(y, (long)a.items + a.tiles);
   const dim3 grid(a.pool.nkv, (unsigned)std::min<long>(std::max<long>(y, 1), 65535));
-  if (use_prompt(a, max_rows)) return launch_kv8_prompt(a, grid, st);
+  if (use_prompt(a.x_bf16, group, max_rows)) return launch_kv8_prompt(a, grid, st);
   if (a.hd == 128) {
     if (nt == 1) launch_cols<128, 1>(a, grid, st);
-    else if (nt == 2) launch_cols<128, 2>(a, grid, st);
-    else launch_cols<128, 4>(a, grid, st);
+    else launch_cols<128, 2>(a, grid, st);
   } else {
     if (nt == 1) launch_cols<64, 1>(a, grid, st);
-    else if (nt == 2) launch_cols<64, 2>(a, grid, st);
-    else launch_cols<64, 4>(a, grid, st);
+    else launch_cols<64, 2>(a, grid, st);
   }
 }
 

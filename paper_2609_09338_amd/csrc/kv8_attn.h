@@ -10,6 +10,8 @@ namespace {
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kNoMax = -1.0e30f;   // below any score: a row that has seen nothing
@@ -36,6 +38,15 @@ OSP_DEV uint32_t word(const uint4* r, int i) {
 OSP_DEV f16x8 frag8(uint32_t a, uint32_t b, float ra = 1.f, float rb = 1.f) {
   return frag(codes_f16(a, false, ra), codes_f16(a, true, ra), codes_f16(b, false, rb), codes_f16(b, true, rb));
 }
+// Eight codes as bf16: the key operand beside bf16 queries, which go in as they are.
+OSP_DEV uint32_t codes_bf16(uint32_t u, bool hi) {
+  return hi ? __builtin_bit_cast(uint32_t, (bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u, 1.f, true))
+            : __builtin_bit_cast(uint32_t, (bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u, 1.f, false));
+}
+OSP_DEV bf16x8 frag8_bf16(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(bf16x8, make_uint4(codes_bf16(a, false), codes_bf16(a, true), codes_bf16(b, false), codes_bf16(b, true)));
+}
+OSP_DEV f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 OSP_DEV f32x4 mfma(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
 // What a block works on.
@@ -51,48 +62,49 @@ OSP_DEV Kv8Seq attn_seq(const Kv8AttnArgs& a, int b) {
   return s;
 }
 
-// Splits of a pass.  split_len: the caller's, or an even deal of the tiles' positions over the
-// items that the launch aims at, no finer than the quantum and no more than n_split a sequence.
-OSP_DEV int plan_len(const Kv8AttnArgs& a, int cols, int group, int quantum, int lane) {
-  if (a.split_len > 0) return a.split_len;
+// The deal of a pass over its items.  Up to 64 sequences are read once, one a lane.
+struct Deal {
+  Kv8Seq mine;    // sequence `lane`
+  int len;        // positions of a split
+};
+OSP_DEV Kv8Seq seq_or_none(const Kv8AttnArgs& a, int b) {
+  Kv8Seq s{0, 0, 0, 0};
+  if (b < a.r.B) s = attn_seq(a, b);
+  return s;
+}
+// split_len: the caller's, or an even deal of the tiles' positions over the items that the launch
+// aims at, no finer than the quantum and no more than n_split a sequence.
+OSP_DEV Deal deal_of(const Kv8AttnArgs& a, int cols, int group, int quantum, int lane) {
+  Deal d;
+  d.mine = seq_or_none(a, lane);
+  d.len = a.split_len;
+  if (d.len > 0) return d;
   float work = 0.f;
   int longest = 1;
   for (int b0 = 0; b0 < a.r.B; b0 += 64) {
-    const int b = b0 + lane;
-    if (b < a.r.B) {
-      const Kv8Seq s = attn_seq(a, b);
-      work += (float)(((s.end - s.beg) * group + cols - 1) / cols) * (float)s.ctx;
-      longest = max(longest, s.ctx);
-    }
+    const Kv8Seq s = b0 == 0 ? d.mine : seq_or_none(a, b0 + lane);
+    work += (float)(((s.end - s.beg) * group + cols - 1) / cols) * (float)s.ctx;
+    longest = max(longest, s.ctx);
   }
-  if (a.r.B > 1) {
-    work = wave_sum(work);
-    longest = wave_max_i(longest);
-  } else {
-    work = lane_f(work, 0);
-    longest = lane_i(longest, 0);
-  }
+  work = wave_sum(work);
+  longest = wave_max_i(longest);
   const float even = work / (float)a.items;
-  int len = even < 1.0e9f ? (int)even + 1 : 1000000000;
-  len = max(len, (longest + a.n_split - 1) / a.n_split);
-  return (len + quantum - 1) / quantum * quantum;
+  d.len = even < 1.0e9f ? (int)even + 1 : 1000000000;
+  d.len = max(d.len, (longest + a.n_split - 1) / a.n_split);
+  d.len = (d.len + quantum - 1) / quantum * quantum;
+  return d;
 }
 
 // Item `it` of the pass: sequences in order, their tiles last to first (the last rows of a prompt
 // see most), a tile's splits in order.  False: there are fewer.
-OSP_DEV bool find_item(const Kv8AttnArgs& a, int it, int len, int cols, int group, int lane, Item& x) {
+OSP_DEV bool find_item(const Kv8AttnArgs& a, const Deal& d, int it, int cols, int group, int lane, Item& x) {
   int before = 0;
   for (int b0 = 0; b0 < a.r.B; b0 += 64) {
-    const int b = b0 + lane;
-    int tiles = 0, ns = 0;
-    if (b < a.r.B) {
-      const Kv8Seq s = attn_seq(a, b);
-      tiles = ((s.end - s.beg) * group + cols - 1) / cols;
-      ns = (s.ctx + len - 1) / len;
-    }
+    const Kv8Seq s = b0 == 0 ? d.mine : seq_or_none(a, b0 + lane);
+    const int tiles = ((s.end - s.beg) * group + cols - 1) / cols, ns = (s.ctx + d.len - 1) / d.len;
     const int n = tiles * ns;
-    const int incl = a.r.B > 1 ? wave_incl_scan<int>(n) : n;
-    const uint64_t past = __builtin_amdgcn_ballot_w64(b < a.r.B && before + incl > it);
+    const int incl = wave_incl_scan<int>(n);
+    const uint64_t past = __builtin_amdgcn_ballot_w64(before + incl > it);
     if (past) {
       const int l = __builtin_ctzll(past);
       x.b = b0 + l;
@@ -100,11 +112,10 @@ OSP_DEV bool find_item(const Kv8AttnArgs& a, int it, int len, int cols, int grou
       const int at = it - before - (lane_i(incl, l) - lane_i(n, l));
       x.tile = lane_i(tiles, l) - 1 - at / x.ns;
       x.split = at % x.ns;
-      x.s = attn_seq(a, x.b);
+      x.s = Kv8Seq{lane_i(s.beg, l), lane_i(s.end, l), lane_i(s.first, l), lane_i(s.ctx, l)};
       return true;
     }
     before += lane_i(incl, 63);
-    if (a.r.B <= 64) break;
   }
   return false;
 }
@@ -179,25 +190,6 @@ OSP_DEV float max4(f32x4 s) { return fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]))
 OSP_DEV int query_exp(float big) {
   const int e = (int)((__float_as_uint(big) >> 23) & 255) - 127;
   return big > 0.f && big < INFINITY ? min(max(13 - e, -114), 120) : 0;
-}
-
-// The lane's HD / 4 dims of a bf16 query vector as B operands (exact); the factor of its scores.
-template <int HD>
-OSP_DEV float query_frags(const bf16_t* p, float scale, f16x8* qf) {
-  float q[HD / 4], big = 0.f;
-#pragma unroll
-  for (int i = 0; i < HD / 4; i += 8) load_vec<bf16_t>(p + i, q + i);
-#pragma unroll
-  for (int i = 0; i < HD / 4; ++i) big = fmaxf(big, fabsf(q[i]));
-  big = fmaxf(big, xor_lane_c(big, 16));
-  big = fmaxf(big, xor_lane_c(big, 32));
-  const int up = query_exp(big);
-  const float f = kv8_pow2(up);
-#pragma unroll
-  for (int c = 0; c < HD / 32; ++c)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) qf[c][j] = (_Float16)(q[c * 8 + j] * f);
-  return kv8_pow2(-up) * (scale * kLog2e);
 }
 
 // P = 2^z of a lane's four exponents as f16; its sum (of the rounded values) joins l.

@@ -5,7 +5,7 @@
 // conversion of the codes need.  A block owns one kv head and 32 NW query vectors (rows x heads
 // of the group), 32 to a wavefront, and walks the split's pages NW / 2 pairs a step:
 //   * each wavefront reads one pair's keys or values (as kv8_attention.hip does), converts them to
-//     f16 once for the whole block and writes them to LDS in the order in which the products' A
+//     bf16 (keys) or f16 (values) once for the whole block and writes them to LDS in the order in which the products' A
 //     operands are read: fragment (K step or dim tile), lane, 8 values.  Reads and writes are
 //     1 KB contiguous per instruction, without bank conflicts.  Two buffers, one barrier a step.
 //   * S^T = K Q^T and O^T += V^T P^T as there, 16x16x32, with the queries and outputs of 32 vectors
@@ -33,16 +33,18 @@ __global__ void __launch_bounds__(64 * NW, 2) k_kv8_prompt(Kv8AttnArgs a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = blockIdx.x, group = a.nq / a.pool.nkv;
   const int n16 = lane & 15, qr = lane >> 4;
-  const int len = plan_len(a, COLS, group, 128, lane);
+  const Deal deal = deal_of(a, COLS, group, 128, lane);
+  const int len = deal.len;
 
   for (int it = blockIdx.y;; it += gridDim.y) {
     Item x;
-    if (!find_item(a, it, len, COLS, group, lane, x)) return;
+    if (!find_item(a, deal, it, COLS, group, lane, x)) return;
     const int nvec = (x.s.end - x.s.beg) * group, c0 = x.tile * COLS + wave * (16 * NT);
 
     // ---- queries and what they see --------------------------------------------------
-    f16x8 qf[NT][KC];
-    float colc[NT], m[NT], l[NT];
+    bf16x8 qf[NT][KC];
+    const float colc = a.scale * kLog2e;
+    float m[NT], l[NT];
     int lim[NT];
     int lim_lo = 0x7fffffff, lim_hi = 0;
     bool missing = false;
@@ -52,7 +54,8 @@ __global__ void __launch_bounds__(64 * NW, 2) k_kv8_prompt(Kv8AttnArgs a) {
       const bool on = c < nvec;
       const int row = x.s.beg + (on ? c / group : 0), h = g * group + (on ? c % group : 0);
       const bf16_t* p = reinterpret_cast<const bf16_t*>(a.q) + (long)row * a.ldq + (long)h * HD + qr * (HD / 4);
-      colc[nt] = query_frags<HD>(p, a.scale, qf[nt]);
+#pragma unroll
+      for (int i = 0; i < KC; ++i) qf[nt][i] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(p + 8 * i));
       Sight see;
       sight_of(a, x, row, on, see, lim_lo, lim_hi, missing);
       lim[nt] = see.lim;
@@ -132,7 +135,7 @@ __global__ void __launch_bounds__(64 * NW, 2) k_kv8_prompt(Kv8AttnArgs a) {
         for (int k = 0; k < 2; ++k)
 #pragma unroll
           for (int c = 0; c < KC; ++c)
-            sm_k[buf][my_pair][k][c][lane] = __builtin_bit_cast(uint4, frag8(word(raw, k * DT + 2 * c), word(raw, k * DT + 2 * c + 1)));
+            sm_k[buf][my_pair][k][c][lane] = __builtin_bit_cast(uint4, frag8_bf16(word(raw, k * DT + 2 * c), word(raw, k * DT + 2 * c + 1)));
       }
     };
 
@@ -176,12 +179,12 @@ __global__ void __launch_bounds__(64 * NW, 2) k_kv8_prompt(Kv8AttnArgs a) {
         // A operands are read four ahead of the products that take them (left to itself the compiler
         // reads one, waits for it and uses it).
         f32x4 sc[NT][2];
-        f16x8 fr[2][4];
+        uint4 fr[2][4];
         const uint4* kp = &sm_k[buf][pr][0][0][lane];
         const uint4* vp = &sm_v[buf][pr][0][lane];
-        auto read4 = [&](f16x8* f, const uint4* p, int at) {
+        auto read4 = [&](uint4* f, const uint4* p, int at) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) f[i] = __builtin_bit_cast(f16x8, p[(at + i) * 64]);
+          for (int i = 0; i < 4; ++i) f[i] = p[(at + i) * 64];
         };
         read4(fr[0], kp, 0);
         __builtin_amdgcn_sched_barrier(0);
@@ -195,14 +198,15 @@ __global__ void __launch_bounds__(64 * NW, 2) k_kv8_prompt(Kv8AttnArgs a) {
 #pragma unroll
           for (int j = 0; j < 4; ++j)
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) sc[nt][(i + j) / KC] = mfma(fr[i / 4 & 1][j], qf[nt][(i + j) % KC], sc[nt][(i + j) / KC]);
+            for (int nt = 0; nt < NT; ++nt) sc[nt][(i + j) / KC] = mfma(__builtin_bit_cast(bf16x8, fr[i / 4 & 1][j]), qf[nt][(i + j) % KC], sc[nt][(i + j) / KC]);
           __builtin_amdgcn_sched_barrier(0);
         }
         if (pr == 0 && s + 1 < n_steps) request(s + 1, ((s + 1) * PAIRS * 2 & 63) == 0 ? id_next : id);
+        const float fa = score_factor(ska, colc), fb = score_factor(skb, colc);
         float z[NT][8], top = -INFINITY;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
-          exponents(sc[nt], score_factor(ska, colc[nt]), score_factor(skb, colc[nt]), kLift - m[nt], z[nt], top);
+          exponents(sc[nt], fa, fb, kLift - m[nt], z[nt], top);
         // One branch for all that is rare: pairs that some vector sees in part, maxima that move.
         if (!whole || __builtin_amdgcn_ballot_w64(top > kLift + kSlack)) {
 #pragma unroll
@@ -212,7 +216,6 @@ __global__ void __launch_bounds__(64 * NW, 2) k_kv8_prompt(Kv8AttnArgs a) {
               mask_scores(sc[nt][0], v, qr);
               mask_scores(sc[nt][1], v >> 16, qr);
             }
-            const float fa = score_factor(ska, colc[nt]), fb = score_factor(skb, colc[nt]);
             float cm = fmaxf(max4(sc[nt][0]) * fa, max4(sc[nt][1]) * fb);
             cm = fmaxf(cm, xor_lane_c(cm, 16));
             cm = fmaxf(cm, xor_lane_c(cm, 32));
@@ -242,7 +245,7 @@ __global__ void __launch_bounds__(64 * NW, 2) k_kv8_prompt(Kv8AttnArgs a) {
 #pragma unroll
           for (int j = 0; j < 4; ++j)
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) acc[nt][i + j] = mfma(fr[f][j], pf[nt], acc[nt][i + j]);
+            for (int nt = 0; nt < NT; ++nt) acc[nt][i + j] = mfma(__builtin_bit_cast(f16x8, fr[f][j]), pf[nt], acc[nt][i + j]);
           __builtin_amdgcn_sched_barrier(0);
         }
       }
