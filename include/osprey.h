@@ -74,7 +74,11 @@ typedef enum {
   OSPREY_E_UNSUPPORTED = -6  /* valid but not implemented (e.g. head_dim other than 64/128) */
 } osprey_status;
 
-typedef enum { OSPREY_F32 = 0, OSPREY_BF16 = 1 } osprey_dtype;
+/* OSPREY_BF16_KV8 (configurations only): bf16 weights, gains and taps, and a KV cache held
+ * in 8 bits as osprey_kv8_cache describes it: half of a bf16 cache's bytes.  Keys and values
+ * are rounded to 4 significant bits; the queries of passes of more than 32 query vectors per
+ * kv head and sequence to bf16.  Every call works as with OSPREY_BF16. */
+typedef enum { OSPREY_F32 = 0, OSPREY_BF16 = 1, OSPREY_BF16_KV8 = 2 } osprey_dtype;
 
 /* Drafter and pool shape.  Weights, norm gains, taps and the KV cache share
  * `dtype`; activations and logits are fp32 throughout. */
@@ -284,7 +288,8 @@ int osprey_config_validate(const osprey_config* cfg);
 
 /* Bytes of the KV pool: kv_num_blocks pages of [n_layers][2][n_kv][kv_block * hd] (dtype);
  * within a page keys are token-major [kv_block][hd] and values dimension-major
- * [hd][kv_block].
+ * [hd][kv_block].  OSPREY_BF16_KV8: pages of codes [n_layers][2][n_kv][16 hd], then the scales
+ * [kv_num_blocks][n_layers][n_kv][2] (the blocks and scales of osprey_kv8_cache).
  * Returns 0 for an invalid configuration. */
 size_t osprey_kv_bytes(const osprey_config* cfg);
 
@@ -529,7 +534,8 @@ int osprey_kv8_keep(const osprey_kv8_cache* c, const osprey_kv8_keep_args* a, vo
  * bit 0 an ingest row count outside [1, max new rows] (pending without verify),
  * bit 1 a token id outside [0, V_T), bit 2 a sequence beyond its KV pages,
  * bit 3 a KV write beyond the slot's pages, bit 4 a draft id outside [0, V_T),
- * bit 5 a tree node whose parent is not an earlier node or the root. */
+ * bit 5 a tree node whose parent is not an earlier node or the root, bit 6 (8-bit caches) a key
+ * or value that is not finite (stored as zero), bit 7 a rotation position outside the table. */
 int osprey_device_errors(osprey_handle* h, uint32_t* flags);
 
 /* Kernel timing for roofline reports.  `families` is a bit mask: bit f enables HIP

@@ -11,7 +11,7 @@ LIB_PATH = os.environ.get("OSPREY_LIB") or os.path.join(_HERE, "libosprey.so")
 
 OSPREY_OK, OSPREY_E_INVALID, OSPREY_E_SHAPE, OSPREY_E_CAPACITY, OSPREY_E_STATE, \
     OSPREY_E_DEVICE, OSPREY_E_UNSUPPORTED = 0, -1, -2, -3, -4, -5, -6
-OSPREY_F32, OSPREY_BF16 = 0, 1
+OSPREY_F32, OSPREY_BF16, OSPREY_BF16_KV8 = 0, 1, 2
 
 STATUS_NAMES = {0: "OK", -1: "E_INVALID", -2: "E_SHAPE", -3: "E_CAPACITY", -4: "E_STATE",
                 -5: "E_DEVICE", -6: "E_UNSUPPORTED"}

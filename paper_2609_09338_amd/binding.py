@@ -103,7 +103,7 @@ class Drafter:
         self.torch = torch
         _check(_lib().osprey_config_validate(C.byref(cfg)))
         dev = d2t.device
-        want = torch.bfloat16 if cfg.dtype == L.OSPREY_BF16 else torch.float32
+        want = torch.float32 if cfg.dtype == L.OSPREY_F32 else torch.bfloat16
         self._wdtype = want
         self.weights = {}
         for k, t in weights.items():

@@ -40,7 +40,8 @@ struct Kv8Pool {
   int nkv;
 };
 
-// The rows of a pass: sequence b has rows [cu[b], cu[b + 1]) (cu nullable: row b), at positions
+// The rows of a pass: sequence b has rows [cu[b], cu[b + 1]) (cu nullable: row b; a single
+// sequence: every row), at positions
 // cached[b] + j, or pos[row] where cached is null (ascending within a sequence; or all alike,
 // rows that see the same context).
 struct Kv8Rows {
@@ -56,7 +57,7 @@ struct Kv8AppendArgs {
   Kv8Pool pool;
   Kv8Rows r;
   const int32_t* rope_pos;  // [rows] (nullable: the row's position)
-  int x_bf16;               // q, k, v and q_out: bf16 (else fp32)
+  int x_bf16;               // q, k, v and q_out: bf16 (else fp32; q_out by q_bf16)
   int g_bf16;               // gains: bf16 (else fp32)
   const void *q, *k, *v;    // row r at + r * ld (elements); heads contiguous (q nullable)
   long ldq, ldk, ldv;
@@ -69,6 +70,7 @@ struct Kv8AppendArgs {
   int max_pos;
   void* q_out;              // row r at + r * ldo: [nq][hd]
   long ldo;
+  int q_bf16;               // fp32 rows: q_out is bf16
   float q_scale;
   uint32_t* err;            // (nullable)
 };
@@ -104,7 +106,7 @@ struct Kv8AttnArgs {
   int32_t* row_ns;          // [rows] splits of each row (written by the attention, read by the merge)
   void* out;                // row r at + r * ldo: [nq][hd]
   long ldo;
-  uint16_t *o_hi, *o_lo;    // or bf16 pairs [rows][nq hd] (nullable)
+  uint16_t *o_hi, *o_lo;    // or bf16 pairs [rows][nq hd] (kv8_prompt.hip, one split; nullable)
   uint32_t* err;
 };
 // Query vectors of one tile of a pass of at most max_rows rows a sequence.
@@ -128,7 +130,7 @@ OSP_DEV Kv8Seq kv8_seq(const Kv8Rows& r, int b) {
   const int total = r.count ? min(*r.count, r.rows) : r.rows;
   Kv8Seq s;
   s.beg = r.cu ? r.cu[b] : b;
-  s.end = r.cu ? r.cu[b + 1] : b + 1;
+  s.end = r.cu ? r.cu[b + 1] : r.B == 1 ? total : b + 1;
   s.beg = min(max(s.beg, 0), total);
   s.end = min(max(s.end, s.beg), total);
   if (r.cached) {

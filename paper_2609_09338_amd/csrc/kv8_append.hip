@@ -181,9 +181,10 @@ OSP_DEV void store_values(uint8_t* blk, const Lanes<HD>& L, int lo, int hi, floa
 }
 
 // The sequence of page unit u: sequence b's units begin at cu[b] / 16 + 2 b, which leaves room
-// for the pages that its rows touch (at most n / 16 + 2); with a row each, unit b is sequence b's.
+// for the pages that its rows touch (at most n / 16 + 2); with a row each, unit b is sequence b's; a single
+// sequence has them all.
 OSP_DEV int unit_seq(const Kv8Rows& r, int u) {
-  if (!r.cu) return u;
+  if (!r.cu) return r.B == 1 ? 0 : u;
   int lo = 0, hi = r.B - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) / 2;
@@ -334,11 +335,15 @@ OSP_DEV void do_queries(const Kv8AppendArgs& a, int row, int h0, int pos, int la
   }
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
-    T* o = reinterpret_cast<T*>(a.q_out) + (long)row * a.ldo + (long)h * HD + k * (HD / 2) + j * V;
+    const long at = (long)row * a.ldo + (long)h * HD + k * (HD / 2) + j * V;
+    T* o = reinterpret_cast<T*>(a.q_out) + at;
     float* y = x + k * V;
     if constexpr (sizeof(T) == 2) {
       *reinterpret_cast<uint4*>(o) = make_uint4(f32x2_to_bf16x2(y[0] * a.q_scale, y[1] * a.q_scale), f32x2_to_bf16x2(y[2] * a.q_scale, y[3] * a.q_scale),
                                                 f32x2_to_bf16x2(y[4] * a.q_scale, y[5] * a.q_scale), f32x2_to_bf16x2(y[6] * a.q_scale, y[7] * a.q_scale));
+    } else if (a.q_bf16) {
+      *reinterpret_cast<uint2*>(reinterpret_cast<bf16_t*>(a.q_out) + at) =
+          make_uint2(f32x2_to_bf16x2(y[0] * a.q_scale, y[1] * a.q_scale), f32x2_to_bf16x2(y[2] * a.q_scale, y[3] * a.q_scale));
     } else {
       *reinterpret_cast<float4*>(o) = make_float4(y[0] * a.q_scale, y[1] * a.q_scale, y[2] * a.q_scale, y[3] * a.q_scale);
     }
@@ -356,7 +361,7 @@ __global__ void __launch_bounds__(256) k_kv8_append(Kv8AppendArgs a, int units, 
     const int b = unit_seq(a.r, u);
     const Kv8Seq s = kv8_seq(a.r, b);
     if (s.end <= s.beg) return;
-    const int pg = s.first / kKv8Page + u - (a.r.cu ? a.r.cu[b] / 16 + 2 * b : b);
+    const int pg = s.first / kKv8Page + u - (a.r.cu ? a.r.cu[b] / 16 + 2 * b : b);   // (b = 0: all of u)
     const int lo = max(s.first, pg * kKv8Page), hi = min(s.first + (s.end - s.beg), (pg + 1) * kKv8Page);
     if (lo >= hi) return;
     const int id = kv8_page(a.pool, b, pg);
@@ -379,7 +384,7 @@ __global__ void __launch_bounds__(256) k_kv8_append(Kv8AppendArgs a, int units, 
   if (a.rope_cos) {
     if (a.rope_pos) pos = a.rope_pos[row];
     else if (a.r.pos) pos = a.r.pos[row];
-    else if (!a.r.cu) pos = a.r.cached[row];
+    else if (!a.r.cu) pos = a.r.B == 1 ? a.r.cached[0] + row : a.r.cached[row];
     else {
       int lo = 0, hi = a.r.B - 1;   // the last sequence that begins at or before the row
       while (lo < hi) {
@@ -491,7 +496,7 @@ __global__ void __launch_bounds__(64) k_kv8_keep(Kv8KeepArgs a) {
 }  // namespace
 
 void launch_kv8_append(const Kv8AppendArgs& a, hipStream_t st) {
-  const int pages = a.r.cu ? a.r.rows / 16 + 2 * a.r.B : a.r.B;
+  const int pages = a.r.cu || a.r.B == 1 ? a.r.rows / 16 + 2 * a.r.B : a.r.B;
   const int units = pages * a.pool.nkv * 2;
   const int hpw = 64 / (a.hd / (2 * (a.x_bf16 ? 8 : 4)));
   const int q_per_row = a.q ? (a.nq + hpw - 1) / hpw : 1;

@@ -264,7 +264,7 @@ __global__ void __launch_bounds__(64 * NW, 2) k_kv8_prompt(Kv8AttnArgs a) {
     if (missing && a.err) atomicOr(a.err, 1u << 2);
 
     // ---- outputs: lane holds dims 16 d + 4 qr .. + 4 of vector n16 of each tile --------
-    const bool direct = x.ns == 1 && a.out != nullptr;
+    const bool direct = x.ns == 1 && (a.out || a.o_hi);   // one split: no join
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       l[nt] += xor_lane_c(l[nt], 16);
@@ -275,7 +275,19 @@ __global__ void __launch_bounds__(64 * NW, 2) k_kv8_prompt(Kv8AttnArgs a) {
       if (h == 0 && qr == 0 && x.split == 0 && a.row_ns) a.row_ns[row] = x.ns;
       if (direct) {
         const float inv = l[nt] > 0.f || l[nt] != l[nt] ? eref / l[nt] : 0.f;
-        bf16_t* o = reinterpret_cast<bf16_t*>(a.out) + (long)row * a.ldo + (long)h * HD + 4 * qr;
+        const long at = (long)row * a.ldo + (long)h * HD + 4 * qr;
+        if (a.o_hi) {
+#pragma unroll
+          for (int d = 0; d < DT; ++d) {
+            uint2 hi, lo;
+            split_bf16x2(acc[nt][d][0] * inv, acc[nt][d][1] * inv, hi.x, lo.x);
+            split_bf16x2(acc[nt][d][2] * inv, acc[nt][d][3] * inv, hi.y, lo.y);
+            *reinterpret_cast<uint2*>(a.o_hi + at + 16 * d) = hi;
+            *reinterpret_cast<uint2*>(a.o_lo + at + 16 * d) = lo;
+          }
+          continue;
+        }
+        bf16_t* o = reinterpret_cast<bf16_t*>(a.out) + at;
 #pragma unroll
         for (int d = 0; d < DT; ++d)
           *reinterpret_cast<uint2*>(o + 16 * d) = make_uint2(f32x2_to_bf16x2(acc[nt][d][0] * inv, acc[nt][d][1] * inv),

@@ -12,6 +12,7 @@
 
 #include "../../include/osprey.h"
 #include "internal.h"
+#include "kv8.h"
 #include "narrow.h"
 
 #define OSPREY_API extern "C" __attribute__((visibility("default")))
@@ -122,8 +123,15 @@ Dims dims_of(const osprey_config& c) {
   return d;
 }
 
+// Bytes of the codes of an 8-bit pool; its scales follow ([block][layer][nkv][2 (k, v)] floats).
+size_t kv8_code_bytes(const osprey_config& c) {
+  return (size_t)c.kv_num_blocks * kv_block_elems(c.n_layers, c.n_kv_heads, c.kv_block, c.head_dim);
+}
+
 // Lays out the workspace; with base == nullptr only returns the size.
-size_t plan(const osprey_config& c, char* base, Ws* w) {
+size_t plan(const osprey_config& cfg, char* base, Ws* w) {
+  osprey_config c = cfg;
+  if (c.dtype == OSPREY_BF16_KV8) c.dtype = OSPREY_BF16;
   const Dims D = dims_of(c);
   size_t off = 0;
   auto take = [&](size_t bytes) -> char* {
@@ -252,7 +260,7 @@ int validate(const osprey_config* c) {
     for (long m : mats)
       if (m * 4 > 0x7fffffffL) return fail(OSPREY_E_UNSUPPORTED, "a weight matrix of %ld values is over 1 GiB in bf16", m);
   }
-  if (c->dtype != OSPREY_F32 && c->dtype != OSPREY_BF16) return fail(OSPREY_E_INVALID, "dtype %d", c->dtype);
+  if (c->dtype != OSPREY_F32 && c->dtype != OSPREY_BF16 && c->dtype != OSPREY_BF16_KV8) return fail(OSPREY_E_INVALID, "dtype %d", c->dtype);
   if (c->qk_norm != 0 && c->qk_norm != 1) return fail(OSPREY_E_INVALID, "qk_norm must be 0 or 1");
   if (!(c->rms_eps > 0.f) || !(c->rope_theta > 1.f)) return fail(OSPREY_E_INVALID, "rms_eps must be > 0 and rope_theta > 1");
   if (c->max_batch < 1 || c->max_batch > kMaxBatch) return fail(OSPREY_E_INVALID, "max_batch %d not in [1, %d]", c->max_batch, kMaxBatch);
@@ -293,7 +301,8 @@ constexpr int kTimedRepeats = 8;
 }  // namespace
 
 struct osprey_handle {
-  osprey_config cfg;
+  osprey_config cfg;    // (dtype: of the weights)
+  bool kv8 = false;     // the cache is held in 8 bits (kv8.h)
   Dims D;
   int n_cu = 1;         // compute units of the device (grid of the LM head)
   osprey_weights w;
@@ -405,7 +414,7 @@ SplitPlan plan_splits(const osprey_handle* h, long ctx_max, long ctx_total, int 
   // Pages that cannot stay in the 256 MB last-level cache from one pass to the next are
   // read non-temporally (faster, and the weights stay cached); a smaller context is
   // read again by every draft step and keeps plain loads.
-  const long el = h->cfg.dtype == OSPREY_BF16 ? 2 : 4;
+  const long el = h->kv8 ? 1 : h->cfg.dtype == OSPREY_BF16 ? 2 : 4;
   p.kv_stream = ctx_total * h->cfg.n_layers * h->cfg.n_kv_heads * h->cfg.head_dim * 2 * el > kKvStreamBytes;
   return p;
 }
@@ -454,6 +463,84 @@ SplitPlan plan_row_splits(const osprey_handle* h, const SplitPlan& sp, int B, in
   return p;
 }
 
+// One layer of an 8-bit pool, as seen by the sequences of a pass (slot0 >= 0: a single one's slot).
+Kv8Pool kv8_pool(const osprey_handle* h, int layer, int slot0, const int32_t* bslot) {
+  const osprey_config& c = h->cfg;
+  const long blk = (long)c.n_kv_heads * c.kv_block * c.head_dim;
+  Kv8Pool p{};
+  p.max_pages = h->D.max_blocks;
+  p.num_pages = c.kv_num_blocks;
+  p.table = h->W.block_table + (slot0 >= 0 ? (long)slot0 * p.max_pages : 0);
+  p.nblocks = h->W.slot_nblocks + std::max(slot0, 0);
+  p.slot = slot0 >= 0 ? nullptr : bslot;
+  p.codes = (uint8_t*)h->kv + 2 * layer * blk;
+  p.page_stride = 2 * c.n_layers * blk;
+  p.scales = (float*)((char*)h->kv + kv8_code_bytes(c)) + 2L * layer * c.n_kv_heads;
+  p.scale_stride = 2L * c.n_layers * c.n_kv_heads;
+  p.nkv = c.n_kv_heads;
+  return p;
+}
+
+// Whether an 8-bit handle's pass attends by tiles of many query vectors, which take bf16 queries
+// (their rounding, 2^-9, is far below the codes', 2^-4; the few rows of a draft step keep fp32).
+bool kv8_many(const AttnArgs& a) { return !a.tree_node && (a.nq / a.nkv) * (long)a.rows_per_seq > 32; }
+
+// launch_rows_qkv of an 8-bit handle (draft-tree rows keep their own bf16 cache).
+void run_rows_qkv(osprey_handle* h, const AttnArgs& a, float* q_out) {
+  if (!h->kv8 || a.tree_node) return launch_rows_qkv(h->cfg.dtype, a, q_out, h->stream);
+  Kv8AppendArgs k{};
+  k.pool = kv8_pool(h, a.layer, a.slot0, a.bslot);
+  k.r = Kv8Rows{a.B, a.rows.max_rows, a.rows.count, a.cu, nullptr, a.rows.pos};
+  k.g_bf16 = 1;
+  const long q_w = a.kv_only ? 0 : (long)a.nq * a.hd;
+  k.q = a.kv_only ? nullptr : a.qkv;
+  k.k = a.qkv + q_w;
+  k.v = a.qkv + q_w + (long)a.nkv * a.hd;
+  k.ldq = k.ldk = k.ldv = a.qkv_w;
+  k.ks = std::max(a.qkv_ks, 1);
+  k.split = a.qkv_split;
+  k.nq = a.kv_only ? 0 : a.nq;
+  k.hd = a.hd;
+  k.q_norm = a.qk_norm ? a.q_norm : nullptr;
+  k.k_norm = a.qk_norm ? a.k_norm : nullptr;
+  k.eps = a.eps;
+  k.rope_cos = a.rope_cos;
+  k.rope_sin = a.rope_sin;
+  k.max_pos = a.max_seq;
+  k.q_out = q_out;
+  k.ldo = (long)a.nq * a.hd;
+  k.q_bf16 = kv8_many(a);
+  k.q_scale = a.scale;
+  k.err = a.err;
+  launch_kv8_append(k, h->stream);
+}
+
+// The attention of an 8-bit handle's pass, into the same partials as the others'.
+void run_kv8_attention(osprey_handle* h, const AttnArgs& a) {
+  Kv8AttnArgs k{};
+  k.pool = kv8_pool(h, a.layer, a.slot0, a.bslot);
+  k.r = Kv8Rows{a.B, a.rows.max_rows, a.rows.count, a.cu, nullptr, a.rows.pos};
+  k.x_bf16 = kv8_many(a);
+  k.q = a.q_prep;
+  k.ldq = k.ldo = (long)a.nq * a.hd;
+  k.nq = a.nq;
+  k.hd = a.hd;
+  k.scale = 1.f;
+  k.n_split = a.n_split;
+  k.split_len = a.split_len;
+  const int cols = kv8_attention_cols(k.x_bf16, a.nq / a.nkv, a.rows_per_seq);
+  k.tiles = (int)((long)a.rows.max_rows * (a.nq / a.nkv) / cols) + a.B;
+  k.stream = a.kv_stream;
+  k.part = a.part;
+  k.natural = 1;
+  if (a.direct) {
+    k.o_hi = a.o_hi;
+    k.o_lo = a.o_lo;
+  }
+  k.err = a.err;
+  launch_kv8_attention(k, a.rows_per_seq, h->stream);
+}
+
 // Attention over the cache and the merge of its context splits.  Timed (family 1),
 // the pair runs kTimedRepeats times back to back between the events: it is idempotent
 // (a new row's keys and values are written again with the same values, every output is
@@ -462,7 +549,8 @@ void run_attention(osprey_handle* h, const AttnArgs& a, bool merge = true, bool 
   const int t = h->t_begin(1);
   const int reps = t >= 0 ? kTimedRepeats : 1;
   for (int rep = 0; rep < reps; ++rep) {
-    if (rows) launch_attention_rows(a, h->stream);
+    if (h->kv8) run_kv8_attention(h, a);
+    else if (rows) launch_attention_rows(a, h->stream);
     else launch_attention(h->cfg.dtype, a, h->stream);
     if (merge && rows && !a.tree_node) launch_attn_join(a, h->stream);
     else if (merge) launch_attn_combine(a, h->stream);
@@ -472,11 +560,14 @@ void run_attention(osprey_handle* h, const AttnArgs& a, bool merge = true, bool 
 
 // Arguments of launch_rows_qkv for rows of which only keys and values are wanted: `qkv`
 // holds their key and value projections alone (kv_w = 2 n_kv hd columns per row).
-void append_args(osprey_handle* h, AttnArgs& a, const RowMeta& rows, const osprey_layer_weights& L, int layer,
-                 int slot0, const int32_t* bslot, const float* qkv, int ks, int kv_w, long split) {
+void append_args(osprey_handle* h, AttnArgs& a, const RowMeta& rows, const int32_t* cu, int B,
+                 const osprey_layer_weights& L, int layer, int slot0, const int32_t* bslot, const float* qkv, int ks,
+                 int kv_w, long split) {
   const osprey_config& c = h->cfg;
   const Ws& W = h->W;
   a.rows = rows;
+  a.cu = cu;
+  a.B = B;
   a.bslot = bslot;
   a.slot0 = slot0;
   a.kv_only = 1;
@@ -555,8 +646,8 @@ bool run_body(osprey_handle* h, RowMeta rows, const int32_t* cu, int B, const fl
       launch_gemv(c.dtype, SRC_QKV, EPI_STORE, kv, h->stream);
       h->t_end(t);
       AttnArgs ka{};
-      append_args(h, ka, rows, L, l, B == 1 ? slot0 : -1, W.bslot, W.qkv, 1, kv.N, 0);
-      launch_rows_qkv(c.dtype, ka, nullptr, h->stream);
+      append_args(h, ka, rows, cu, B, L, l, B == 1 ? slot0 : -1, W.bslot, W.qkv, 1, kv.N, 0);
+      run_rows_qkv(h, ka, nullptr);
       if (keep == 0) return true;
       KeepArgs k{};
       k.n = keep;
@@ -623,6 +714,10 @@ bool run_body(osprey_handle* h, RowMeta rows, const int32_t* cu, int B, const fl
     // A single row's O projection merges the context splits while it stages its input
     // (one launch fewer per layer); otherwise the merge kernel writes o.
     const bool merge_in_o = gemv_attn_supported(c.dtype, rows.max_rows, nq * hd, hd, sp.n_split);
+    if (h->kv8) {
+      run_rows_qkv(h, a, W.o);
+      a.q_prep = W.o;
+    }
     run_attention(h, a, !merge_in_o);
     // O projection + residual
     GemvArgs go{};
@@ -773,8 +868,8 @@ bool run_body_mr(osprey_handle* h, RowMeta rows, const int32_t* cu, int B, const
       const int ks = gemm(SRC_PREP, EPI_STORE, g);
       h->t_end(t);
       AttnArgs a{};
-      append_args(h, a, rows, L, l, (B == 1 && !tree) ? slot0 : -1, W.bslot, part, ks, g.N, (long)rows.max_rows * g.N);
-      launch_rows_qkv(c.dtype, a, nullptr, h->stream);
+      append_args(h, a, rows, cu, B, L, l, (B == 1 && !tree) ? slot0 : -1, W.bslot, part, ks, g.N, (long)rows.max_rows * g.N);
+      run_rows_qkv(h, a, nullptr);
       if (keep == 0) return true;
       KeepArgs k{};
       k.n = keep;
@@ -863,14 +958,15 @@ bool run_body_mr(osprey_handle* h, RowMeta rows, const int32_t* cu, int B, const
     // row per sequence (draft steps), or a few rows of a single sequence (the ingest at
     // batch 1): the attention blocks sum the QKV partials and prepare their own queries,
     // one launch fewer per layer.
-    const bool own_prep = rows_per_seq == 1 || (B == 1 && rows_per_seq <= kOwnPrepRows);
+    // (8-bit caches: a block's scale needs all of its new tokens, so one kernel writes them.)
+    const bool own_prep = !h->kv8 && (rows_per_seq == 1 || (B == 1 && rows_per_seq <= kOwnPrepRows));
     if (!own_prep || tree) {
-      launch_rows_qkv(c.dtype, a, W.o, h->stream);
+      run_rows_qkv(h, a, W.o);
       a.q_prep = W.o;
     }
     // Sequences of more than 16 prepared query vectors per kv head walk their pages once per
     // block of vectors instead of once per 16 vectors (attention_rows.hip).
-    const bool by_rows = a.q_prep && attn_rows_supported(c.dtype, rows_per_seq, nq / nkv);
+    const bool by_rows = h->kv8 ? kv8_many(a) : a.q_prep && attn_rows_supported(c.dtype, rows_per_seq, nq / nkv);
     if (by_rows) {
       const SplitPlan rp = plan_row_splits(h, sp, B, rows_per_seq, rows.max_rows, tree != nullptr);
       a.n_split = rp.n_split;
@@ -1161,6 +1257,8 @@ OSPREY_API int osprey_config_validate(const osprey_config* cfg) { return validat
 
 OSPREY_API size_t osprey_kv_bytes(const osprey_config* c) {
   if (validate(c) != OSPREY_OK) return 0;
+  if (c->dtype == OSPREY_BF16_KV8)
+    return kv8_code_bytes(*c) + (size_t)c->kv_num_blocks * c->n_layers * c->n_kv_heads * 2 * sizeof(float);
   const size_t el = c->dtype == OSPREY_BF16 ? 2 : 4;
   return (size_t)c->kv_num_blocks * kv_block_elems(c->n_layers, c->n_kv_heads, c->kv_block, c->head_dim) * el;
 }
@@ -1198,6 +1296,8 @@ OSPREY_API int osprey_draft_init(const osprey_config* cfg, const osprey_weights*
 
   osprey_handle* h = new osprey_handle();
   h->cfg = *cfg;
+  h->kv8 = cfg->dtype == OSPREY_BF16_KV8;
+  if (h->kv8) h->cfg.dtype = OSPREY_BF16;
   h->D = dims_of(*cfg);
   h->n_cu = n_cu;
   h->w = *w;
@@ -1291,7 +1391,24 @@ OSPREY_API int osprey_kv_append(osprey_handle* h, int32_t slot, int32_t n, const
   if (s.len_max + n > (long)s.nblocks * h->cfg.kv_block)
     return fail(OSPREY_E_CAPACITY, "slot %d: %ld + %d positions exceed its %d pages", slot, s.len_max, n, s.nblocks);
   if (n == 0) return ok();
-  launch_kv_append(h->cfg.dtype, h->kv, k, v, h->cfg.n_layers, n, h->cfg.n_kv_heads, h->cfg.head_dim,
+  if (h->kv8) {
+    const osprey_config& c = h->cfg;
+    const long layer = (long)n * c.n_kv_heads * c.head_dim;
+    Kv8AppendArgs q{};
+    q.r = Kv8Rows{1, n, nullptr, nullptr, h->W.slot_len + slot, nullptr};
+    q.x_bf16 = 1;
+    q.ldk = q.ldv = (long)c.n_kv_heads * c.head_dim;
+    q.ks = 1;
+    q.hd = c.head_dim;
+    q.err = h->W.err;
+    for (int l = 0; l < c.n_layers; ++l) {
+      q.pool = kv8_pool(h, l, slot, nullptr);
+      q.k = (const uint16_t*)k + l * layer;
+      q.v = (const uint16_t*)v + l * layer;
+      launch_kv8_append(q, h->stream);
+    }
+  }
+  launch_kv_append(h->cfg.dtype, h->kv, k, v, h->kv8 ? 0 : h->cfg.n_layers, n, h->cfg.n_kv_heads, h->cfg.head_dim,
                    h->cfg.kv_block, h->W.block_table, slot, h->D.max_blocks, h->W.slot_len,
                    h->W.slot_len, h->stream);
   s.len_max += n;

@@ -46,7 +46,8 @@ def capacity(w, ctx: int, n_iters: int) -> int:
     return int(ctx) + (n_iters + 1) * (w.K + 1) + 2 * w.K + 1
 
 
-def make_drafter(w, n_iters: int, device="cuda:0", weights=None) -> Setup:
+def make_drafter(w, n_iters: int, device="cuda:0", weights=None, kv8: bool = False) -> Setup:
+    """kv8: the cache held in 8 bits (bf16 workloads)."""
     import torch
     weights = synth.make_weights(w) if weights is None else weights
     d2t = synth.make_d2t(w)
@@ -59,7 +60,7 @@ def make_drafter(w, n_iters: int, device="cuda:0", weights=None) -> Setup:
                       n_kv_heads=w.n_kv_heads, head_dim=w.head_dim, d_ffn=w.d_ffn,
                       vocab_draft=w.vocab_draft, vocab_target=w.vocab_target,
                       target_hidden=w.target_hidden, n_taps=w.n_taps,
-                      dtype=L.OSPREY_BF16 if w.dtype == "bf16" else L.OSPREY_F32,
+                      dtype=L.OSPREY_F32 if w.dtype == "f32" else L.OSPREY_BF16_KV8 if kv8 else L.OSPREY_BF16,
                       qk_norm=w.qk_norm, rms_eps=w.rms_eps, rope_theta=w.rope_theta,
                       max_batch=w.batch, max_k=w.K, max_seq_len=max(caps),
                       kv_block=w.kv_block, kv_num_blocks=int(sum(nblk)),

@@ -155,3 +155,13 @@ def test_attention_of_one_position_returns_its_value_and_of_none_zeros():
     sees = torch.tensor([[True, False], [False, False]])
     o, _ = R.attention(ref, 0, torch.ones((2, 1, 64)), sees, 0.1, 0.0, 0.0)
     assert torch.equal(o[0, 0], ref.read(0, 0)[1][0]) and bool((o[1] == 0).all())
+
+
+def test_an_8_bit_configuration_is_valid_and_its_pool_about_half(lib):  # noqa: F811
+    from paper_2609_09338_amd import binding as bd
+    from .test_abi_cpu import _cfg
+    assert bd.config_validate(_cfg(dtype=2)) == 0
+    codes = bd.kv_bytes(_cfg()) // 2
+    assert bd.kv_bytes(_cfg(dtype=2)) == codes + 256 * 2 * 8 * 2 * 4   # a scale per page, layer, head, keys and values
+    assert bd.workspace_bytes(_cfg(dtype=2)) == bd.workspace_bytes(_cfg())
+    assert bd.config_validate(_cfg(dtype=3)) == INVALID
