@@ -302,57 +302,190 @@ OSP_DEV void append_values(const Kv8AppendArgs& a, int r0, int off, int n, int g
   if (lane == 0) *scale = kv8_pow2(e);
 }
 
-// Queries: HPW heads a wavefront, HD / (2 V) lanes a head, V values of either half a lane.
-template <typename T, int HD>
-OSP_DEV void do_queries(const Kv8AppendArgs& a, int row, int h0, int pos, int lane) {
+// Position of a row, for its rotation.
+OSP_DEV int rope_row(const Kv8AppendArgs& a, int row) {
+  if (!a.rope_cos) return 0;
+  if (a.rope_pos) return a.rope_pos[row];
+  if (a.r.pos) return a.r.pos[row];
+  if (!a.r.cu) return a.r.B == 1 ? a.r.cached[0] + row : a.r.cached[row];
+  int lo = 0, hi = a.r.B - 1;   // the last sequence that begins at or before the row
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) / 2;
+    if (a.r.cu[mid] <= row) lo = mid;
+    else hi = mid - 1;
+  }
+  return a.r.cached[lo] + row - a.r.cu[lo];
+}
+
+// Queries of RQ rows from row0 on: HD / (2 V) lanes a head, V values of either half a lane; every
+// row's values are requested before the first is used.
+template <typename T, int HD, int RQ>
+OSP_DEV void do_queries(const Kv8AppendArgs& a, int row0, int rows, int h0, int lane) {
   constexpr int V = Vec<T>::N, LPH = HD / (2 * V);
   const int h = h0 + lane / LPH, j = lane % LPH;
   if (h >= a.nq) return;   // (whole groups of lanes that reduce together)
-  float x[2 * V];
+  float xs[RQ][2 * V];
+  int pos[RQ];
 #pragma unroll
-  for (int k = 0; k < 2; ++k)
-    load_n<T, V>(a.q, (long)row * a.ldq + (long)h * HD + k * (HD / 2) + j * V, a.ks, a.split, x + k * V);
-  if (a.q_norm) {
-    float ss = 0.f;
+  for (int r = 0; r < RQ; ++r) {
+    const int row = min(row0 + r, rows - 1);
 #pragma unroll
-    for (int i = 0; i < 2 * V; ++i) ss += x[i] * x[i];
-    ss += dpp_f<kDppXor1>(ss);
-    ss += dpp_f<kDppXor2>(ss);
-    if constexpr (LPH >= 8) ss += dpp_f<kDppHalfMirror>(ss);
-    if constexpr (LPH >= 16) ss += dpp_f<kDppMirror>(ss);
-    const float inv = 1.0f / sqrtf(ss / HD + a.eps);
-#pragma unroll
-    for (int i = 0; i < 2 * V; ++i) x[i] *= inv * gain(a.q_norm, a.g_bf16, (i / V) * (HD / 2) + j * V + i % V);
+    for (int k = 0; k < 2; ++k)
+      load_n<T, V>(a.q, (long)row * a.ldq + (long)h * HD + k * (HD / 2) + j * V, a.ks, a.split, xs[r] + k * V);
   }
-  if (a.rope_cos) {
-    const long c = (long)min(max(pos, 0), a.max_pos - 1) * (HD / 2) + j * V;
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const float co = a.rope_cos[c + i], si = a.rope_sin[c + i], u = x[i], w = x[V + i];
-      x[i] = u * co - w * si;
-      x[V + i] = w * co + u * si;
+  for (int r = 0; r < RQ; ++r) pos[r] = rope_row(a, min(row0 + r, rows - 1));
+#pragma unroll
+  for (int r = 0; r < RQ; ++r) {
+    const int row = row0 + r;
+    if (row >= rows) return;
+    float* x = xs[r];
+    if (a.q_norm) {
+      float ss = 0.f;
+#pragma unroll
+      for (int i = 0; i < 2 * V; ++i) ss += x[i] * x[i];
+      ss += dpp_f<kDppXor1>(ss);
+      ss += dpp_f<kDppXor2>(ss);
+      if constexpr (LPH >= 8) ss += dpp_f<kDppHalfMirror>(ss);
+      if constexpr (LPH >= 16) ss += dpp_f<kDppMirror>(ss);
+      const float inv = 1.0f / sqrtf(ss / HD + a.eps);
+#pragma unroll
+      for (int i = 0; i < 2 * V; ++i) x[i] *= inv * gain(a.q_norm, a.g_bf16, (i / V) * (HD / 2) + j * V + i % V);
     }
-  }
+    if (a.rope_cos) {
+      const long c = (long)min(max(pos[r], 0), a.max_pos - 1) * (HD / 2) + j * V;
 #pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const long at = (long)row * a.ldo + (long)h * HD + k * (HD / 2) + j * V;
-    T* o = reinterpret_cast<T*>(a.q_out) + at;
-    float* y = x + k * V;
-    if constexpr (sizeof(T) == 2) {
-      *reinterpret_cast<uint4*>(o) = make_uint4(f32x2_to_bf16x2(y[0] * a.q_scale, y[1] * a.q_scale), f32x2_to_bf16x2(y[2] * a.q_scale, y[3] * a.q_scale),
-                                                f32x2_to_bf16x2(y[4] * a.q_scale, y[5] * a.q_scale), f32x2_to_bf16x2(y[6] * a.q_scale, y[7] * a.q_scale));
-    } else if (a.q_bf16) {
-      *reinterpret_cast<uint2*>(reinterpret_cast<bf16_t*>(a.q_out) + at) =
-          make_uint2(f32x2_to_bf16x2(y[0] * a.q_scale, y[1] * a.q_scale), f32x2_to_bf16x2(y[2] * a.q_scale, y[3] * a.q_scale));
-    } else {
-      *reinterpret_cast<float4*>(o) = make_float4(y[0] * a.q_scale, y[1] * a.q_scale, y[2] * a.q_scale, y[3] * a.q_scale);
+      for (int i = 0; i < V; ++i) {
+        const float co = a.rope_cos[c + i], si = a.rope_sin[c + i], u = x[i], w = x[V + i];
+        x[i] = u * co - w * si;
+        x[V + i] = w * co + u * si;
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const long at = (long)row * a.ldo + (long)h * HD + k * (HD / 2) + j * V;
+      T* o = reinterpret_cast<T*>(a.q_out) + at;
+      float* y = x + k * V;
+      if constexpr (sizeof(T) == 2) {
+        *reinterpret_cast<uint4*>(o) = make_uint4(f32x2_to_bf16x2(y[0] * a.q_scale, y[1] * a.q_scale), f32x2_to_bf16x2(y[2] * a.q_scale, y[3] * a.q_scale),
+                                                  f32x2_to_bf16x2(y[4] * a.q_scale, y[5] * a.q_scale), f32x2_to_bf16x2(y[6] * a.q_scale, y[7] * a.q_scale));
+      } else if (a.q_bf16) {
+        *reinterpret_cast<uint2*>(reinterpret_cast<bf16_t*>(a.q_out) + at) =
+            make_uint2(f32x2_to_bf16x2(y[0] * a.q_scale, y[1] * a.q_scale), f32x2_to_bf16x2(y[2] * a.q_scale, y[3] * a.q_scale));
+      } else {
+        *reinterpret_cast<float4*>(o) = make_float4(y[0] * a.q_scale, y[1] * a.q_scale, y[2] * a.q_scale, y[3] * a.q_scale);
+      }
     }
   }
 }
+// The rows that queries are formed for: those of the sequences.
+OSP_DEV int query_rows(const Kv8AppendArgs& a) {
+  const int total = a.r.count ? min(*a.r.count, a.r.rows) : a.r.rows;
+  return a.r.cu ? min(total, a.r.cu[a.r.B]) : total;
+}
 
-// Wavefronts [0, units): blocks of the cache; the rest: queries.
+// One new token a sequence: a wavefront owns the token's key and value of one kv head, a rotation
+// pair of dims (l, l + hd / 2) a lane.  (k_kv8_append holds a page's sixteen tokens; for one it runs
+// 16 KB of code once.)  Older codes are touched where the scale grows.
 template <typename T, int HD>
-__global__ void __launch_bounds__(256) k_kv8_append(Kv8AppendArgs a, int units, int q_per_row) {
+__global__ void __launch_bounds__(256) k_kv8_append_one(Kv8AppendArgs a, int units, int q_per_row) {
+  constexpr int H = HD / 2, ND = HD / 32;
+  const int lane = threadIdx.x & 63;
+  const int w = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+  if (w >= units) {
+    const int rows = query_rows(a), row = (w - units) / q_per_row;
+    if (row < rows) do_queries<T, HD, 1>(a, row, rows, ((w - units) % q_per_row) * (64 / (HD / (2 * Vec<T>::N))), lane);
+    return;
+  }
+  const int g = w % a.pool.nkv, b = w / a.pool.nkv;
+  const Kv8Seq s = kv8_seq(a.r, b);
+  if (s.end <= s.beg) return;
+  const int row = s.beg, e0 = lane % H, pg = s.first / kKv8Page, off = s.first % kKv8Page;
+  const T *kp = reinterpret_cast<const T*>(a.k) + (long)row * a.ldk + (long)g * HD, *vp = reinterpret_cast<const T*>(a.v) + (long)row * a.ldv + (long)g * HD;
+  float f[4] = {load_f32(kp, e0), load_f32(kp, e0 + H), load_f32(vp, e0), load_f32(vp, e0 + H)};
+  for (int k = 1; k < a.ks; ++k) {
+    f[0] += load_f32(kp, e0 + k * a.split);
+    f[1] += load_f32(kp, e0 + H + k * a.split);
+    f[2] += load_f32(vp, e0 + k * a.split);
+    f[3] += load_f32(vp, e0 + H + k * a.split);
+  }
+  float co = 1.f, si = 0.f;
+  if (a.rope_cos) {
+    const int p = a.rope_pos ? a.rope_pos[row] : s.first;
+    if ((p < 0 || p >= a.max_pos) && a.err) atomicOr(a.err, 1u << 7);
+    const long c = (long)min(max(p, 0), a.max_pos - 1) * H + e0;
+    co = a.rope_cos[c];
+    si = a.rope_sin[c];
+  }
+  const int id = kv8_page(a.pool, b, pg);
+  if (id < 0) {
+    if (lane == 0 && a.err) atomicOr(a.err, 1u << 3);
+    return;
+  }
+  uint8_t* kb = a.pool.codes + (long)id * a.pool.page_stride + (long)g * (kKv8Page * HD);
+  uint8_t* vb = kb + (long)a.pool.nkv * (kKv8Page * HD);
+  float* sc = a.pool.scales + (long)id * a.pool.scale_stride + 2 * g;
+  const float was_k = sc[0], was_v = sc[1];
+  double x0 = f[0], x1 = f[1];
+  if (a.k_norm) {
+    double ss = lane < H ? x0 * x0 + x1 * x1 : 0.0;
+    ss = wave_sum_d(ss);
+    const double inv = 1.0 / sqrt(ss / HD + (double)a.eps);
+    x0 *= inv * (double)gain(a.k_norm, a.g_bf16, e0);
+    x1 *= inv * (double)gain(a.k_norm, a.g_bf16, e0 + H);
+  }
+  const double y0 = x0 * (double)co - x1 * (double)si, y1 = x1 * (double)co + x0 * (double)si;
+  double kv[2] = {y0, y1};
+  bool bad = false;
+  double kmax = 0.0;
+  float vmax = 0.f;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    if (!(fabs(kv[i]) < 1.0e300)) { kv[i] = 0.0; bad = true; }
+    if (!(fabsf(f[2 + i]) < INFINITY)) { f[2 + i] = 0.f; bad = true; }
+    kmax = fmax(kmax, fabs(kv[i]));
+    vmax = fmaxf(vmax, fabsf(f[2 + i]));
+  }
+  if (bad && a.err) atomicOr(a.err, 1u << 6);
+  kmax = wave_max_d(kmax);
+  vmax = wave_max(vmax);
+  const int wk = off > 0 ? exp_of(was_k) : kKv8MinExp, wv = off > 0 ? exp_of(was_v) : kKv8MinExp;
+  const int ek = max(scale_exp(kmax), wk), ev = max(scale_exp((double)vmax), wv);
+  if (off > 0 && ek > wk) shift_keys<HD>(kb, Lanes<HD>(lane), off, kv8_pow2(max(wk - ek, -126)));
+  if (off > 0 && ev > wv) {
+    // (the new token's byte too: written below)
+    const float r = kv8_pow2(max(wv - ev, -126));
+    uint32_t* p = reinterpret_cast<uint32_t*>(vb);
+    for (int i = lane; i < 4 * HD; i += 64) {
+      const int live = min(max(off - 4 * (i / HD), 0), 4);   // older tokens of the four
+      const uint32_t old = p[i], below = live >= 4 ? 0xffffffffu : (1u << 8 * live) - 1u;
+      if (live > 0) p[i] = (shift4(old, r) & below) | (old & ~below);
+    }
+  }
+  if (lane < H) {
+    const double rk = __longlong_as_double((long long)(1023 - ek) << 52);
+    const float r0 = kv8_pow2(-ev / 2), r1 = kv8_pow2(-ev - (-ev / 2));
+    const uint32_t ku = pack4(to_float_odd(kv[0] * rk), to_float_odd(kv[1] * rk), 0.f, 0.f);
+    const uint32_t vu = pack4(f[2] * r0 * r1, f[3] * r0 * r1, 0.f, 0.f);
+    kb[off * HD + e0] = (uint8_t)ku;
+    kb[off * HD + e0 + H] = (uint8_t)(ku >> 8);
+    // the dword store above and this byte may come from different lanes
+    __builtin_amdgcn_s_waitcnt(0);
+    uint8_t* vt = vb + (off / 4) * 4 * HD + off % 4;
+    vt[(e0 % 16) * (HD / 4) + (e0 / 16) * 4] = (uint8_t)vu;
+    vt[(e0 % 16) * (HD / 4) + (e0 / 16 + ND) * 4] = (uint8_t)(vu >> 8);
+  }
+  if (lane == 0) {
+    sc[0] = kv8_pow2(ek);
+    sc[1] = kv8_pow2(ev);
+  }
+}
+
+// Wavefronts [0, units): blocks of the cache; the rest: queries, one row each or (many) four.
+constexpr int kQueryRows = 4;
+constexpr long kManyQueries = 4 * 256 * 16;
+template <typename T, int HD>
+__global__ void __launch_bounds__(256) k_kv8_append(Kv8AppendArgs a, int units, int q_per_row, int many) {
   const int lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
   if (w < units) {
@@ -376,26 +509,12 @@ __global__ void __launch_bounds__(256) k_kv8_append(Kv8AppendArgs a, int units, 
     else append_values<T, HD>(a, r0, off, hi - lo, g, blk, sc, lane);
     return;
   }
-  const int v = w - units;
-  const int row = v / q_per_row, h0 = (v % q_per_row) * (64 / (HD / (2 * Vec<T>::N)));
-  const int total = a.r.count ? min(*a.r.count, a.r.rows) : a.r.rows;
-  if (row >= total || (a.r.cu && row >= a.r.cu[a.r.B])) return;   // behind the last sequence
-  int pos = 0;
-  if (a.rope_cos) {
-    if (a.rope_pos) pos = a.rope_pos[row];
-    else if (a.r.pos) pos = a.r.pos[row];
-    else if (!a.r.cu) pos = a.r.B == 1 ? a.r.cached[0] + row : a.r.cached[row];
-    else {
-      int lo = 0, hi = a.r.B - 1;   // the last sequence that begins at or before the row
-      while (lo < hi) {
-        const int mid = (lo + hi + 1) / 2;
-        if (a.r.cu[mid] <= row) lo = mid;
-        else hi = mid - 1;
-      }
-      pos = a.r.cached[lo] + row - a.r.cu[lo];
-    }
+  const int v = w - units, h0 = (v % q_per_row) * (64 / (HD / (2 * Vec<T>::N))), rows = query_rows(a);
+  if (many) {
+    if (v / q_per_row * kQueryRows < rows) do_queries<T, HD, kQueryRows>(a, v / q_per_row * kQueryRows, rows, h0, lane);
+  } else if (v / q_per_row < rows) {
+    do_queries<T, HD, 1>(a, v / q_per_row, rows, h0, lane);
   }
-  do_queries<T, HD>(a, row, h0, pos, lane);
 }
 
 // One wavefront per (sequence, kv head, keys or values): the positions base .. base + n - 1 take
@@ -495,19 +614,32 @@ __global__ void __launch_bounds__(64) k_kv8_keep(Kv8KeepArgs a) {
 
 }  // namespace
 
-void launch_kv8_append(const Kv8AppendArgs& a, hipStream_t st) {
-  const int pages = a.r.cu || a.r.B == 1 ? a.r.rows / 16 + 2 * a.r.B : a.r.B;
-  const int units = pages * a.pool.nkv * 2;
-  const int hpw = 64 / (a.hd / (2 * (a.x_bf16 ? 8 : 4)));
+template <typename T, int HD>
+void launch_append(const Kv8AppendArgs& a, hipStream_t st) {
+  constexpr int hpw = 64 / (HD / (2 * Vec<T>::N));   // heads a wavefront
   const int q_per_row = a.q ? (a.nq + hpw - 1) / hpw : 1;
-  const long waves = units + (a.q ? (long)a.r.rows * q_per_row : 0);
-  const dim3 grid((unsigned)((waves + 3) / 4));
+  const bool one = !a.r.cu && (a.r.B > 1 || a.r.rows == 1);
+  if (one) {
+    const int units = a.r.B * a.pool.nkv;
+    const long waves = units + (a.q ? (long)a.r.rows * q_per_row : 0);
+    hipLaunchKernelGGL((k_kv8_append_one<T, HD>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, st, a, units, q_per_row);
+    return;
+  }
+  const int units = (a.r.rows / 16 + 2 * a.r.B) * a.pool.nkv * 2;
+  const long q_waves = a.q ? (long)a.r.rows * q_per_row : 0;
+  // Four rows a wavefront where that still fills the chip (256 CUs of 16 such wavefronts).
+  const int many = q_waves >= kManyQueries;
+  const long waves = units + (many ? (long)((a.r.rows + kQueryRows - 1) / kQueryRows) * q_per_row : q_waves);
+  hipLaunchKernelGGL((k_kv8_append<T, HD>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, st, a, units, q_per_row, many);
+}
+
+void launch_kv8_append(const Kv8AppendArgs& a, hipStream_t st) {
   if (a.x_bf16) {
-    if (a.hd == 128) hipLaunchKernelGGL((k_kv8_append<bf16_t, 128>), grid, dim3(256), 0, st, a, units, q_per_row);
-    else hipLaunchKernelGGL((k_kv8_append<bf16_t, 64>), grid, dim3(256), 0, st, a, units, q_per_row);
+    if (a.hd == 128) launch_append<bf16_t, 128>(a, st);
+    else launch_append<bf16_t, 64>(a, st);
   } else {
-    if (a.hd == 128) hipLaunchKernelGGL((k_kv8_append<float, 128>), grid, dim3(256), 0, st, a, units, q_per_row);
-    else hipLaunchKernelGGL((k_kv8_append<float, 64>), grid, dim3(256), 0, st, a, units, q_per_row);
+    if (a.hd == 128) launch_append<float, 128>(a, st);
+    else launch_append<float, 64>(a, st);
   }
 }
 
