@@ -427,57 +427,61 @@ class Kv8Cache:
         self.c = L.osprey_kv8_cache(_ptr(page_table), self.batch, int(page_table.shape[1]), pages, nkv, head_dim,
                                     _ptr(codes), codes.stride(0) if pages > 1 else 2 * nkv * w, _ptr(scales),
                                     scales.stride(0) if pages > 1 else 2 * nkv)
+        self.ref = C.byref(self.c)
 
 
 def _same_device(*tensors):
-    dev = tensors[0].device
+    dev = tensors[0].get_device()
     for t in tensors:
-        if t is not None and (t.device != dev or not t.is_cuda):
-            raise ValueError(f"need tensors of one GPU, got {dev} and {t.device}")
-    return dev
+        if t is not None and t.get_device() != dev or dev < 0:
+            raise ValueError(f"need tensors of one GPU, got {tensors[0].device} and {t.device}")
+    return tensors[0].device
 
 
 def _ints(t, numel: int, name: str):
-    import torch
-    if t is not None and (t.dtype != torch.int32 or not t.is_contiguous() or t.numel() < numel):
+    """The address of at least numel contiguous int32 (None: NULL)."""
+    if t is None:
+        return None
+    if t.dtype is not _torch().int32 or not t.is_contiguous() or t.numel() < numel:
         raise ValueError(f"{name}: need {numel} contiguous int32, got {t.dtype} {tuple(t.shape)}")
-    return t
+    return t.data_ptr()
 
 
 def _heads(t, rows: int, hd: int, dtype, name: str) -> int:
     """The row stride of [rows, heads, hd] whose heads are contiguous."""
-    if t.dim() != 3 or t.dtype != dtype or t.shape[0] != rows or t.shape[2] != hd:
-        raise ValueError(f"{name}: need {dtype} [{rows}, heads, {hd}], got {t.dtype} {tuple(t.shape)}")
-    if t.stride(2) != 1 or (t.stride(1) != hd and t.shape[1] > 1):
+    sh = t.shape
+    if len(sh) != 3 or t.dtype is not dtype or sh[0] != rows or sh[2] != hd:
+        raise ValueError(f"{name}: need {dtype} [{rows}, heads, {hd}], got {t.dtype} {tuple(sh)}")
+    st = t.stride()
+    if st[2] != 1 or (st[1] != hd and sh[1] > 1):
         raise ValueError(f"{name}: the heads of a row must be contiguous")
-    return t.stride(0) if rows > 1 else t.shape[1] * hd
+    return st[0] if rows > 1 else sh[1] * hd
+
+
+def _torch():
+    import torch
+    return torch
 
 
 def _kv8_dtype(t) -> int:
-    import torch
-    if t.dtype == torch.bfloat16:
+    torch = _torch()
+    if t.dtype is torch.bfloat16:
         return L.OSPREY_BF16
-    if t.dtype == torch.float32:
+    if t.dtype is torch.float32:
         return L.OSPREY_F32
     raise ValueError(f"dtype {t.dtype}: need bfloat16 or float32")
 
 
-class _on:
-    """The device of a call's buffers as the current one, and the stream to enqueue on."""
-
-    def __init__(self, device, stream):
-        import torch
-        self.guard = torch.cuda.device(device) if device.index != torch.cuda.current_device() else None
-        self.stream = stream if stream is not None else torch.cuda.current_stream(device)
-
-    def __enter__(self):
-        if self.guard:
-            self.guard.__enter__()
-        return C.c_void_p(self.stream.cuda_stream)
-
-    def __exit__(self, *e):
-        if self.guard:
-            self.guard.__exit__(*e)
+def _kv8_call(fn, cache, a, stream) -> None:
+    """Enqueue on `stream`, or the current stream of the cache's device, with that device current."""
+    torch = _torch()
+    st = stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(cache.device.index)
+    if torch.cuda.current_device() == cache.device.index:
+        rc = fn(cache.ref, C.byref(a), st)
+    else:
+        with torch.cuda.device(cache.device):
+            rc = fn(cache.ref, C.byref(a), st)
+    _check(rc)
 
 
 def kv8_append(cache: Kv8Cache, k, v, cached, q=None, q_out=None, cu_rows=None, rope_pos=None, q_norm=None, k_norm=None,
@@ -487,41 +491,36 @@ def kv8_append(cache: Kv8Cache, k, v, cached, q=None, q_out=None, cu_rows=None, 
     into q_out, normalised per head where a gain is given and rotated where rope_cos / rope_sin
     [positions, head_dim / 2] are.  cu_rows int32 [batch + 1] groups the rows (None: one row
     per sequence).  errors: an int32 device word whose bits the kernels set."""
-    import torch
-    rows, hd, dt = int(k.shape[0]), cache.head_dim, k.dtype
-    a = L.osprey_kv8_append_args()
-    a.dtype = _kv8_dtype(k)
+    rows, hd, dt = k.shape[0], cache.head_dim, k.dtype
+    dtype = _kv8_dtype(k)
     _same_device(cache.codes, k, v, cached, q, q_out, cu_rows, rope_pos, q_norm, k_norm, rope_cos, rope_sin, errors)
-    a.rows = rows
-    a.k_stride, a.v_stride = _heads(k, rows, hd, dt, "k"), _heads(v, rows, hd, dt, "v")
+    ks, vs, qs, os = _heads(k, rows, hd, dt, "k"), _heads(v, rows, hd, dt, "v"), 0, 0
     if k.shape[1] != cache.n_kv_heads or v.shape[1] != cache.n_kv_heads:
         raise ValueError(f"k and v: need {cache.n_kv_heads} heads")
-    a.k, a.v = _ptr(k), _ptr(v)
     if q is not None:
         if q_out is None or q_out.shape != q.shape:
             raise ValueError("q_out: need a tensor of q's shape")
-        a.q, a.q_stride, a.q_out, a.q_out_stride = _ptr(q), _heads(q, rows, hd, dt, "q"), _ptr(q_out), _heads(q_out, rows, hd, dt, "q_out")
-        a.n_q_heads = int(q.shape[1])
+        qs, os = _heads(q, rows, hd, dt, "q"), _heads(q_out, rows, hd, dt, "q_out")
     for t, name in ((q_norm, "q_norm"), (k_norm, "k_norm")):
-        if t is not None and (t.dtype != dt or t.numel() != hd or not t.is_contiguous()):
+        if t is not None and (t.dtype is not dt or t.numel() != hd or not t.is_contiguous()):
             raise ValueError(f"{name}: need {hd} contiguous {dt}")
-    a.q_norm, a.k_norm, a.eps = _ptr(q_norm), _ptr(k_norm), eps
     if rope_cos is not None:
         for t in (rope_cos, rope_sin):
-            if t is None or t.dtype != torch.float32 or t.dim() != 2 or t.shape[1] != hd // 2 or not t.is_contiguous() \
+            if t is None or t.dtype is not _torch().float32 or t.dim() != 2 or t.shape[1] != hd // 2 or not t.is_contiguous() \
                     or t.shape != rope_cos.shape:
                 raise ValueError(f"rope_cos and rope_sin: need contiguous float32 [positions, {hd // 2}] of one shape")
-        a.rope_cos, a.rope_sin, a.rope_len = _ptr(rope_cos), _ptr(rope_sin), int(rope_cos.shape[0])
-    a.cu_rows, a.cached = _ptr(_ints(cu_rows, cache.batch + 1, "cu_rows")), _ptr(_ints(cached, cache.batch, "cached"))
-    a.rope_pos, a.err = _ptr(_ints(rope_pos, rows, "rope_pos")), _ptr(_ints(errors, 1, "errors"))
-    with _on(cache.device, stream) as st:
-        _check(_lib().osprey_kv8_append(C.byref(cache.c), C.byref(a), st))
+    a = L.osprey_kv8_append_args(
+        rows, _ints(cu_rows, cache.batch + 1, "cu_rows"), _ints(cached, cache.batch, "cached"), _ints(rope_pos, rows, "rope_pos"), dtype,
+        0 if q is None else q.shape[1], _ptr(q), k.data_ptr(), v.data_ptr(), qs, ks, vs, _ptr(q_norm), _ptr(k_norm), eps, _ptr(rope_cos),
+        _ptr(rope_sin), 0 if rope_cos is None else rope_cos.shape[0], None if q is None else q_out.data_ptr(), os,
+        _ints(errors, 1, "errors"))
+    _kv8_call(_lib().osprey_kv8_append, cache, a, stream)
 
 
 def kv8_attention_workspace(cache: Kv8Cache, rows: int, n_q_heads: int, max_rows: int, max_context: int) -> int:
     """Bytes of the workspace of a kv8_attention call with these sizes."""
-    with _on(cache.device, None):
-        n = int(_lib().osprey_kv8_workspace_bytes(C.byref(cache.c), rows, n_q_heads, max_rows, max_context))
+    with _torch().cuda.device(cache.device):
+        n = int(_lib().osprey_kv8_workspace_bytes(cache.ref, rows, n_q_heads, max_rows, max_context))
     if n == 0:
         raise OspreyError(L.OSPREY_E_INVALID, last_error())
     return n
@@ -533,27 +532,20 @@ def kv8_attention(cache: Kv8Cache, q, out, cached, workspace, max_rows: int = 1,
     see of the cache (their own positions already appended).  tree_mask int64 [rows, 2]: the
     bits of the new positions that a row sees.  max_rows, max_context: the largest row count and
     context the call is planned for.  workspace: uint8, kv8_attention_workspace bytes."""
-    import torch
-    rows, hd, dt = int(q.shape[0]), cache.head_dim, q.dtype
-    a = L.osprey_kv8_attention_args()
-    a.dtype = _kv8_dtype(q)
+    torch = _torch()
+    rows, hd, dt = q.shape[0], cache.head_dim, q.dtype
     _same_device(cache.codes, q, out, cached, workspace, cu_rows, tree_mask, errors)
-    a.rows, a.max_rows, a.max_context = rows, int(max_rows), int(max_context)
     if out.shape != q.shape:
         raise ValueError("out: need a tensor of q's shape")
-    a.q, a.q_stride, a.out, a.out_stride = _ptr(q), _heads(q, rows, hd, dt, "q"), _ptr(out), _heads(out, rows, hd, dt, "out")
-    a.n_q_heads = int(q.shape[1])
-    a.scale = hd ** -0.5 if scale is None else scale
-    if tree_mask is not None and (tree_mask.dtype != torch.int64 or tuple(tree_mask.shape) != (rows, 2) or not tree_mask.is_contiguous()):
+    if tree_mask is not None and (tree_mask.dtype is not torch.int64 or tuple(tree_mask.shape) != (rows, 2) or not tree_mask.is_contiguous()):
         raise ValueError(f"tree_mask: need a contiguous int64 [{rows}, 2]")
-    a.tree_mask = _ptr(tree_mask)
-    if workspace.dtype != torch.uint8 or not workspace.is_contiguous():
+    if workspace.dtype is not torch.uint8 or not workspace.is_contiguous():
         raise ValueError("workspace: need a contiguous uint8 tensor")
-    a.workspace, a.workspace_bytes = _ptr(workspace), workspace.numel()
-    a.cu_rows, a.cached = _ptr(_ints(cu_rows, cache.batch + 1, "cu_rows")), _ptr(_ints(cached, cache.batch, "cached"))
-    a.err = _ptr(_ints(errors, 1, "errors"))
-    with _on(cache.device, stream) as st:
-        _check(_lib().osprey_kv8_attention(C.byref(cache.c), C.byref(a), st))
+    a = L.osprey_kv8_attention_args(
+        rows, max_rows, max_context, _ints(cu_rows, cache.batch + 1, "cu_rows"), _ints(cached, cache.batch, "cached"), _ptr(tree_mask),
+        _kv8_dtype(q), q.shape[1], q.data_ptr(), _heads(q, rows, hd, dt, "q"), hd ** -0.5 if scale is None else scale, out.data_ptr(),
+        _heads(out, rows, hd, dt, "out"), workspace.data_ptr(), workspace.numel(), _ints(errors, 1, "errors"))
+    _kv8_call(_lib().osprey_kv8_attention, cache, a, stream)
 
 
 def kv8_keep(cache: Kv8Cache, base, path, n, errors=None, stream=None) -> None:
@@ -561,10 +553,9 @@ def kv8_keep(cache: Kv8Cache, base, path, n, errors=None, stream=None) -> None:
     _same_device(cache.codes, base, path, n, errors)
     if path.dim() != 2 or path.shape[0] != cache.batch:
         raise ValueError(f"path: need [{cache.batch}, nodes]")
-    a = L.osprey_kv8_keep_args(_ptr(_ints(base, cache.batch, "base")), _ptr(_ints(path, path.numel(), "path")), int(path.shape[1]),
-                               _ptr(_ints(n, cache.batch, "n")), _ptr(_ints(errors, 1, "errors")))
-    with _on(cache.device, stream) as st:
-        _check(_lib().osprey_kv8_keep(C.byref(cache.c), C.byref(a), st))
+    a = L.osprey_kv8_keep_args(_ints(base, cache.batch, "base"), _ints(path, path.numel(), "path"), path.shape[1],
+                               _ints(n, cache.batch, "n"), _ints(errors, 1, "errors"))
+    _kv8_call(_lib().osprey_kv8_keep, cache, a, stream)
 
 
 class IterationGraph:
