@@ -103,24 +103,24 @@ int compute_units() {
 constexpr int kSplitQuantum = 128;
 
 struct AttnPlan {
-  int n_split, tiles, items;
+  int n_split, tiles, items, by_units;
   size_t ns_bytes, part_bytes;
 };
-AttnPlan attention_plan(int batch, int nkv, int hd, int rows, int nq, int x_bf16, int max_rows, int max_context, int n_cu) {
+AttnPlan attention_plan(int batch, int nkv, int hd, int rows, int nq, int x_bf16, int max_rows, int max_context, int max_pages,
+                        int n_cu) {
   AttnPlan p{};
   const int cols = kv8_attention_cols(x_bf16, nq / nkv, max_rows);
   p.tiles = (int)((long)rows * (nq / nkv) / cols) + batch;
   // as many blocks as can be resident: eight wavefronts per CU
-  #ifndef A_ITEMS
-#define A_ITEMS 2
-#endif
-  const int per_cu = cols == kKv8PromptCols ? 2 : A_ITEMS;
-  p.items = std::max(1, (per_cu * n_cu + nkv - 1) / nkv);
+    p.items = std::max(1, (2 * n_cu + nkv - 1) / nkv);
   p.n_split = (int)std::min<long>(kKv8MaxSplits, std::max(1L, ((long)max_context + kSplitQuantum - 1) / kSplitQuantum));
   // (a pass that fills the chip with its tiles is not cut)
   if ((long)rows * (nq / nkv) / cols >= p.items) p.n_split = 1;
+  // (splits by units may begin anywhere in a sequence: one more; their count fits an int)
+  p.by_units = p.n_split > 1 && cols != kKv8PromptCols && (long)p.tiles * (max_pages / 8 + 1) < 1L << 30;
+  if (p.by_units) p.n_split = std::min(p.n_split + 1, kKv8MaxSplits);
   if (p.n_split > 1) {
-    p.ns_bytes = ((size_t)rows * 4 + 255) & ~size_t(255);
+    p.ns_bytes = ((size_t)rows * nq * 4 + 255) & ~size_t(255);
     p.part_bytes = (size_t)rows * nq * p.n_split * (hd + 2) * 4;
   }
   return p;
@@ -191,7 +191,7 @@ OSPREY_API size_t osprey_kv8_workspace_bytes(const osprey_kv8_cache* c, int32_t 
   }
   size_t need = 256;
   for (int bf16 = 0; bf16 < 2; ++bf16) {   // (of either type of rows)
-    const AttnPlan p = attention_plan(c->batch, c->n_kv_heads, c->head_dim, rows, n_q_heads, bf16, max_rows, max_context, n_cu);
+    const AttnPlan p = attention_plan(c->batch, c->n_kv_heads, c->head_dim, rows, n_q_heads, bf16, max_rows, max_context, c->max_pages, n_cu);
     need = std::max(need, p.ns_bytes + p.part_bytes);
   }
   report_error(OSPREY_OK, "");
@@ -215,7 +215,7 @@ OSPREY_API int osprey_kv8_attention(const osprey_kv8_cache* c, const osprey_kv8_
   const int n_cu = compute_units();
   if (n_cu < 1) return fail(OSPREY_E_DEVICE, "no HIP device");
   const AttnPlan p = attention_plan(c->batch, c->n_kv_heads, c->head_dim, a->rows, a->n_q_heads, a->dtype == OSPREY_BF16,
-                                    a->max_rows, a->max_context, n_cu);
+                                    a->max_rows, a->max_context, c->max_pages, n_cu);
   if (p.part_bytes > 0) {
     if (!a->workspace || ((uintptr_t)a->workspace & 15)) return fail(OSPREY_E_INVALID, "workspace must be non-NULL and 16-byte aligned");
     if (a->workspace_bytes < p.ns_bytes + p.part_bytes)
@@ -234,6 +234,7 @@ OSPREY_API int osprey_kv8_attention(const osprey_kv8_cache* c, const osprey_kv8_
   k.tree = a->tree_mask;
   k.n_split = p.n_split;
   k.items = p.items;
+  k.by_units = p.by_units;
   k.tiles = p.tiles;
   // (a last-level cache of 256 MB: contexts beyond it are not read again soon)
   k.stream = (long)c->batch * a->max_context * c->n_kv_heads * c->head_dim * 2 > (160L << 20);

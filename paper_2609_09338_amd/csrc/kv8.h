@@ -98,12 +98,13 @@ struct Kv8AttnArgs {
   const uint64_t* tree;     // [rows][2] bit i: the row sees position cached + i (nullable: causal)
   int n_split;              // partials per row and head
   int split_len;            // positions per split (0: planned on the device from the lengths)
-  int items;                // blocks of column tiles x splits that the plan aims at
+  int by_units;             // the work is dealt by units of positions across sequences (kv8_attn.h)
+  int items;                // blocks per kv head that the plan aims at
   int tiles;                // host bound on the column tiles of all sequences
   int stream;               // pages are read once: non-temporal loads
   float* part;              // [rows][nq][n_split][hd + 2]: max, sum, unnormalised output
   int natural;              // part's maxima in natural units (else log2)
-  int32_t* row_ns;          // [rows] splits of each row (written by the attention, read by the merge)
+  int32_t* row_ns;          // [rows][nq] splits of each output (written by the attention, read by the merge)
   void* out;                // row r at + r * ldo: [nq][hd]
   long ldo;
   uint16_t *o_hi, *o_lo;    // or bf16 pairs [rows][nq hd] (kv8_prompt.hip, one split; nullable)

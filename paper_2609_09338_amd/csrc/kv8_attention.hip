@@ -54,36 +54,38 @@ template <int HD> struct Page {
   OSP_DEV uint32_t vd(int i) const { return word(v, i); }
 };
 
-constexpr int NP_(bool f) { return f ? 2 : 1; }
 template <int HD, int NT, bool F32, bool STREAM>
-#ifndef A_OCC
-#define A_OCC 2
-#endif
-__global__ void __launch_bounds__(256, (NT * NP_(F32) <= 2 ? A_OCC : 1)) k_kv8_attn(Kv8AttnArgs a) {
+__global__ void __launch_bounds__(256, (NT == 1 || !F32 ? 2 : 1)) k_kv8_attn(Kv8AttnArgs a) {
   constexpr int KC = HD / 32;         // K steps of the score product
   constexpr int DT = HD / 16;         // 16-row tiles of dims
   constexpr int NP = F32 ? 2 : 1;     // parts of Q and P
-#ifndef A_DEPTH
-#define A_DEPTH 2
-#endif
-  constexpr int DEPTH = NT * NP == 1 ? A_DEPTH : 2;   // pairs in flight
+  constexpr int DEPTH = 2;            // pairs in registers
   constexpr int COLS = 16 * NT;
   __shared__ float sm_o[4][COLS][HD + 4];
   __shared__ float sm_m[4][COLS], sm_l[4][COLS];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = blockIdx.x, group = a.nq / a.pool.nkv;
   const int n16 = lane & 15, qr = lane >> 4;
-  const Deal deal = deal_of(a, COLS, group, 128, lane);
-  const int len = deal.len;
+  const Deal deal = deal_of(a, COLS, group, lane);
+  int at = deal.units ? blockIdx.y * deal.len : blockIdx.y;      // a unit, or an item
+  const int at_end = deal.units ? min(at + deal.len, deal.units) : 0;
 
-  for (int it = blockIdx.y;; it += gridDim.y) {
+  for (;;) {
     Item x;
-    if (!find_item(a, deal, it, COLS, group, lane, x)) return;
+    if (deal.units) {
+      if (at >= at_end) return;
+      int used;
+      find_piece(a, deal, at, at_end, COLS, group, lane, x, used);
+      at += used;
+    } else {
+      if (!find_item(a, deal, at, COLS, group, lane, x)) return;
+      at += gridDim.y;
+    }
     const int nvec = (x.s.end - x.s.beg) * group, c0 = x.tile * COLS;
 
     // ---- the split's page pairs: wave, wave + 4, ... ---------------------------------
     // Requested before anything else: the first pages, then the queries, then the scales.
-    const int p_lo = x.split * len, s_hi = min(p_lo + len, x.s.ctx);
+    const int p_lo = x.lo, s_hi = x.hi;
     const long k_off = (long)g * (kKv8Page * HD) + n16 * HD + qr * (HD / 4);
     const long v_off = (long)(a.pool.nkv + g) * (kKv8Page * HD) + qr * 4 * HD + n16 * (HD / 4);
     // 32 of the wavefront's pairs at a time, a page a lane (-1: none, -2: not in the split)
@@ -326,7 +328,7 @@ __global__ void __launch_bounds__(256, (NT * NP_(F32) <= 2 ? A_OCC : 1)) k_kv8_a
         o[3] += v.w * f;
       }
       const int row = x.s.beg + c / group, h = g * group + c % group;
-      if (e == 0 && h == 0 && x.split == 0 && a.row_ns) a.row_ns[row] = x.ns;
+      if (e == 0 && x.split == 0 && a.row_ns) a.row_ns[(long)row * a.nq + h] = x.ns;
       if (direct) {
         const float inv = L > 0.f || L != L ? 1.f / L : 0.f;
         const long at = (long)row * a.ldo + (long)h * HD + e;
@@ -361,7 +363,7 @@ __global__ void __launch_bounds__(256) k_kv8_join(Kv8AttnArgs a) {
   const int row = i / a.nq, h = i % a.nq;
   const int total = a.r.count ? min(*a.r.count, a.r.rows) : a.r.rows;
   const bool on = row < total && !(a.r.cu && row >= a.r.cu[a.r.B]);
-  const int ns = on ? min(a.row_ns[row], a.n_split) : 0;
+  const int ns = on ? min(a.row_ns[i], a.n_split) : 0;
   float o[E] = {}, L = 0.f;
   if (ns > 1) {   // (else written by the attention itself)
     const float* pp = a.part + ((long)row * a.nq + h) * a.n_split * (HD + 2);
@@ -434,7 +436,8 @@ int kv8_attention_cols(int x_bf16, int group, int max_rows) {
 void launch_kv8_attention(const Kv8AttnArgs& a, int max_rows, hipStream_t st) {
   const int group = a.nq / a.pool.nkv, nt = cols_nt(group, max_rows);
   long y = (long)a.tiles * a.n_split;
-  if (a.split_len == 0 && a.n_split > 1) y = std::min<long>(y, (long)a.items + a.tiles);
+  if (a.by_units) y = a.items;
+  else if (a.split_len == 0 && a.n_split > 1) y = std::min<long>(y, (long)a.items + a.tiles);
   const dim3 grid(a.pool.nkv, (unsigned)std::min<long>(std::max<long>(y, 1), 65535));
   if (use_prompt(a.x_bf16, group, max_rows)) return launch_kv8_prompt(a, grid, st);
   if (a.hd == 128) {

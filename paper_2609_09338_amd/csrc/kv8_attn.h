@@ -53,6 +53,7 @@ OSP_DEV f32x4 mfma(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32
 struct Item {
   Kv8Seq s;
   int b, tile, split, ns;
+  int lo, hi;     // positions
 };
 
 // Rows of sequence b and what they can see: no more than its table holds.
@@ -62,37 +63,106 @@ OSP_DEV Kv8Seq attn_seq(const Kv8AttnArgs& a, int b) {
   return s;
 }
 
-// The deal of a pass over its items.  Up to 64 sequences are read once, one a lane.
+// The deal of a pass.  Up to 64 sequences are read once, one a lane.
+//   by splits  an item is one split of `len` positions of one tile
+//   by units   (where a.by_units allows it) the tiles' contexts lie end to end in units of kUnit positions, and every
+//              block takes the same number of them, whichever sequences they fall in: a block that is
+//              left with a whole split of a long sequence reads alone at the end (64 sequences of 512
+//              to 4095 positions by splits: 80 us)
+constexpr int kUnit = 128;
 struct Deal {
   Kv8Seq mine;    // sequence `lane`
-  int len;        // positions of a split
+  int len;        // positions of a split, or units of a block
+  int units;      // by units: all of them (else 0)
 };
 OSP_DEV Kv8Seq seq_or_none(const Kv8AttnArgs& a, int b) {
   Kv8Seq s{0, 0, 0, 0};
   if (b < a.r.B) s = attn_seq(a, b);
   return s;
 }
+OSP_DEV int tiles_of(const Kv8Seq& s, int cols, int group) { return ((s.end - s.beg) * group + cols - 1) / cols; }
+OSP_DEV int units_of(const Kv8Seq& s) { return (s.ctx + kUnit - 1) / kUnit; }
+
 // split_len: the caller's, or an even deal of the tiles' positions over the items that the launch
-// aims at, no finer than the quantum and no more than n_split a sequence.
-OSP_DEV Deal deal_of(const Kv8AttnArgs& a, int cols, int group, int quantum, int lane) {
+// aims at, no finer than a unit and no more than n_split a sequence.
+OSP_DEV Deal deal_of(const Kv8AttnArgs& a, int cols, int group, int lane) {
   Deal d;
   d.mine = seq_or_none(a, lane);
   d.len = a.split_len;
+  d.units = 0;
   if (d.len > 0) return d;
   float work = 0.f;
-  int longest = 1;
+  int longest = 1, units = 0;
   for (int b0 = 0; b0 < a.r.B; b0 += 64) {
     const Kv8Seq s = b0 == 0 ? d.mine : seq_or_none(a, b0 + lane);
-    work += (float)(((s.end - s.beg) * group + cols - 1) / cols) * (float)s.ctx;
+    if (a.by_units) units += tiles_of(s, cols, group) * units_of(s);
+    else work += (float)tiles_of(s, cols, group) * (float)s.ctx;
     longest = max(longest, s.ctx);
   }
-  work = wave_sum(work);
   longest = wave_max_i(longest);
+  if (a.by_units) {
+    units = lane_i(wave_incl_scan<int>(units), 63);
+    const int even = (units + a.items - 1) / a.items;
+    // By splits where they come out even: a split a block, at most a quarter longer than the even deal
+    // (a second piece costs a block about as much as two or three units).
+#pragma unroll 1
+    for (int k = 0; k < 3; ++k) {
+      const int len = even * (8 + k) / 8, whole = (longest + kUnit - 1) / kUnit;
+      if ((whole + len - 1) / len > a.n_split) continue;
+      int n = 0;
+      for (int b0 = 0; b0 < a.r.B; b0 += 64) {
+        const Kv8Seq s = b0 == 0 ? d.mine : seq_or_none(a, b0 + lane);
+        n += tiles_of(s, cols, group) * ((units_of(s) + len - 1) / len);
+      }
+      if (lane_i(wave_incl_scan<int>(n), 63) <= a.items) {
+        d.len = len * kUnit;
+        return d;
+      }
+    }
+    d.units = units;
+    d.len = even;
+    // (a tile may begin and end inside a block's range: one split more)
+    d.len = max(d.len, ((longest + kUnit - 1) / kUnit + a.n_split - 2) / (a.n_split - 1));
+    return d;
+  }
+  work = wave_sum(work);
   const float even = work / (float)a.items;
   d.len = even < 1.0e9f ? (int)even + 1 : 1000000000;
   d.len = max(d.len, (longest + a.n_split - 1) / a.n_split);
-  d.len = (d.len + quantum - 1) / quantum * quantum;
+  d.len = (d.len + kUnit - 1) / kUnit * kUnit;
   return d;
+}
+
+// By units: what lies at unit p of a block's range [.., end): a piece of one tile, positions
+// [x.lo, x.hi), `used` units long.
+OSP_DEV void find_piece(const Kv8AttnArgs& a, const Deal& d, int p, int end, int cols, int group, int lane, Item& x, int& used) {
+  int before = 0;
+  for (int b0 = 0; b0 < a.r.B; b0 += 64) {
+    const Kv8Seq s = b0 == 0 ? d.mine : seq_or_none(a, b0 + lane);
+    const int tiles = tiles_of(s, cols, group), u = units_of(s), n = tiles * u;
+    const int incl = wave_incl_scan<int>(n);
+    const uint64_t past = __builtin_amdgcn_ballot_w64(before + incl > p);
+    if (past) {
+      const int l = __builtin_ctzll(past), ul = lane_i(u, l);
+      const int at = p - before - (lane_i(incl, l) - lane_i(n, l)), t = at / ul, o = at % ul;
+      const int begin = p - o;                      // where the tile begins
+      used = min(ul - o, end - p);
+      x.b = b0 + l;
+      x.tile = lane_i(tiles, l) - 1 - t;
+      x.split = p / d.len - begin / d.len;
+      x.ns = (begin + ul - 1) / d.len - begin / d.len + 1;
+      x.s = Kv8Seq{lane_i(s.beg, l), lane_i(s.end, l), lane_i(s.first, l), lane_i(s.ctx, l)};
+      x.lo = o * kUnit;
+      x.hi = min((o + used) * kUnit, x.s.ctx);
+      return;
+    }
+    before += lane_i(incl, 63);
+  }
+  used = end - p;   // (not reached: p < units)
+  x.lo = x.hi = 0;
+  x.tile = x.split = x.b = 0;
+  x.ns = 1;
+  x.s = Kv8Seq{0, 0, 0, 0};
 }
 
 // Item `it` of the pass: sequences in order, their tiles last to first (the last rows of a prompt
@@ -101,7 +171,7 @@ OSP_DEV bool find_item(const Kv8AttnArgs& a, const Deal& d, int it, int cols, in
   int before = 0;
   for (int b0 = 0; b0 < a.r.B; b0 += 64) {
     const Kv8Seq s = b0 == 0 ? d.mine : seq_or_none(a, b0 + lane);
-    const int tiles = ((s.end - s.beg) * group + cols - 1) / cols, ns = (s.ctx + d.len - 1) / d.len;
+    const int tiles = tiles_of(s, cols, group), ns = (s.ctx + d.len - 1) / d.len;
     const int n = tiles * ns;
     const int incl = wave_incl_scan<int>(n);
     const uint64_t past = __builtin_amdgcn_ballot_w64(before + incl > it);
@@ -113,6 +183,8 @@ OSP_DEV bool find_item(const Kv8AttnArgs& a, const Deal& d, int it, int cols, in
       x.tile = lane_i(tiles, l) - 1 - at / x.ns;
       x.split = at % x.ns;
       x.s = Kv8Seq{lane_i(s.beg, l), lane_i(s.end, l), lane_i(s.first, l), lane_i(s.ctx, l)};
+      x.lo = x.split * d.len;
+      x.hi = min(x.lo + d.len, x.s.ctx);
       return true;
     }
     before += lane_i(incl, 63);

@@ -33,8 +33,7 @@ __global__ void __launch_bounds__(64 * NW, 2) k_kv8_prompt(Kv8AttnArgs a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = blockIdx.x, group = a.nq / a.pool.nkv;
   const int n16 = lane & 15, qr = lane >> 4;
-  const Deal deal = deal_of(a, COLS, group, 128, lane);
-  const int len = deal.len;
+  const Deal deal = deal_of(a, COLS, group, lane);
 
   for (int it = blockIdx.y;; it += gridDim.y) {
     Item x;
@@ -73,7 +72,7 @@ __global__ void __launch_bounds__(64 * NW, 2) k_kv8_prompt(Kv8AttnArgs a) {
 #pragma unroll
       for (int d = 0; d < DT; ++d) acc[nt][d] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    const int p_lo = x.split * len, p_hi = min(p_lo + len, t_hi);
+    const int p_lo = x.lo, p_hi = min(x.hi, t_hi);
     const int n_pairs = p_hi > p_lo ? (p_hi - p_lo + 31) / 32 : 0;
     const int n_steps = (n_pairs + PAIRS - 1) / PAIRS;
     // this wavefront's part of a step: keys or values of pair `wave % PAIRS`
@@ -272,7 +271,7 @@ __global__ void __launch_bounds__(64 * NW, 2) k_kv8_prompt(Kv8AttnArgs a) {
       const int c = c0 + 16 * nt + n16;
       if (c >= nvec) continue;
       const int row = x.s.beg + c / group, h = g * group + c % group;
-      if (h == 0 && qr == 0 && x.split == 0 && a.row_ns) a.row_ns[row] = x.ns;
+      if (qr == 0 && x.split == 0 && a.row_ns) a.row_ns[(long)row * a.nq + h] = x.ns;
       if (direct) {
         const float inv = l[nt] > 0.f || l[nt] != l[nt] ? eref / l[nt] : 0.f;
         const long at = (long)row * a.ldo + (long)h * HD + 4 * qr;
