@@ -425,7 +425,8 @@ int osprey_graph_destroy(osprey_graph* g);
  * (OCP: finite, magnitudes up to 448), scales powers of two, value = code * scale.  Within a
  * block keys are [16][head_dim] and values [4][16][head_dim / 16][4]: token t, dim e at
  * [t / 4][e % 16][e / 16][t % 4].  Strides let one pool hold the pages of several layers.
- * A page belongs to one sequence.  Memory need not be cleared: no call reads a position that
+ * A page that is written belongs to one sequence; pages that are only read may be shared.
+ * Memory need not be cleared: no call reads a position that
  * was not written, but what a caller writes there itself must be finite codes.
  *
  * Device conditions (err, nullable, a device word that the calls only set bits of): bit 2 a

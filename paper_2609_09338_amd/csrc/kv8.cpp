@@ -101,6 +101,7 @@ int compute_units() {
 }
 
 constexpr int kSplitQuantum = 128;
+constexpr long kPartBytes = 256L << 20;
 
 struct AttnPlan {
   int n_split, tiles, items, by_units;
@@ -114,8 +115,15 @@ AttnPlan attention_plan(int batch, int nkv, int hd, int rows, int nq, int x_bf16
   // as many blocks as can be resident: eight wavefronts per CU
     p.items = std::max(1, (2 * n_cu + nkv - 1) / nkv);
   p.n_split = (int)std::min<long>(kKv8MaxSplits, std::max(1L, ((long)max_context + kSplitQuantum - 1) / kSplitQuantum));
-  // (a pass that fills the chip with its tiles is not cut)
-  if ((long)rows * (nq / nkv) / cols >= p.items) p.n_split = 1;
+  // A pass that fills the chip with its tiles is not cut.  The partials of others take 256 MB at most,
+  // or what twice the even deal needs: enough for one long context among many short ones.
+  const long full = (long)rows * (nq / nkv) / cols;
+  if (full >= p.items) {
+    p.n_split = 1;
+  } else if (rows > 0) {
+    const long room = kPartBytes / ((long)rows * nq * (hd + 2) * 4);
+    p.n_split = (int)std::min<long>(p.n_split, std::max(room, 2L * p.items / std::max(full, 1L) + 2));
+  }
   // (splits by units may begin anywhere in a sequence: one more; their count fits an int)
   p.by_units = p.n_split > 1 && cols != kKv8PromptCols && (long)p.tiles * (max_pages / 8 + 1) < 1L << 30;
   if (p.by_units) p.n_split = std::min(p.n_split + 1, kKv8MaxSplits);
@@ -133,6 +141,7 @@ OSPREY_API int osprey_kv8_append(const osprey_kv8_cache* c, const osprey_kv8_app
   if (rc) return rc;
   if (!a) return fail(OSPREY_E_INVALID, "the arguments are NULL");
   if ((rc = check_rows(c, a->rows, a->cu_rows, a->cached))) return rc;
+  if (a->rows == 0) return report_error(OSPREY_OK, "");   // nothing to do
   if (a->dtype != OSPREY_F32 && a->dtype != OSPREY_BF16) return fail(OSPREY_E_INVALID, "dtype %d", a->dtype);
   if ((rc = check_buffer("k", a->k, a->k_stride, c->n_kv_heads, c->head_dim, a->dtype))) return rc;
   if ((rc = check_buffer("v", a->v, a->v_stride, c->n_kv_heads, c->head_dim, a->dtype))) return rc;
@@ -148,7 +157,6 @@ OSPREY_API int osprey_kv8_append(const osprey_kv8_cache* c, const osprey_kv8_app
   if ((a->q_norm || a->k_norm) && !(a->eps > 0.f && std::isfinite(a->eps))) return fail(OSPREY_E_INVALID, "eps must be > 0");
   if (!a->rope_cos != !a->rope_sin) return fail(OSPREY_E_INVALID, "rope_cos and rope_sin go together");
   if (a->rope_cos && a->rope_len < 1) return fail(OSPREY_E_INVALID, "rope_len %d", a->rope_len);
-  if (a->rows == 0) return report_error(OSPREY_OK, "");
   Kv8AppendArgs k{};
   k.pool = pool_of(c);
   k.r = Kv8Rows{c->batch, a->rows, nullptr, a->cu_rows, a->cached, nullptr};
@@ -203,6 +211,7 @@ OSPREY_API int osprey_kv8_attention(const osprey_kv8_cache* c, const osprey_kv8_
   if (rc) return rc;
   if (!a) return fail(OSPREY_E_INVALID, "the arguments are NULL");
   if ((rc = check_rows(c, a->rows, a->cu_rows, a->cached))) return rc;
+  if (a->rows == 0) return report_error(OSPREY_OK, "");   // nothing to do
   if ((rc = check_heads(c, a->n_q_heads, a->rows))) return rc;
   if (a->dtype != OSPREY_F32 && a->dtype != OSPREY_BF16) return fail(OSPREY_E_INVALID, "dtype %d", a->dtype);
   if (a->max_rows < 1 || a->max_context < 1)
@@ -221,7 +230,6 @@ OSPREY_API int osprey_kv8_attention(const osprey_kv8_cache* c, const osprey_kv8_
     if (a->workspace_bytes < p.ns_bytes + p.part_bytes)
       return fail(OSPREY_E_CAPACITY, "workspace_bytes %zu < %zu", a->workspace_bytes, p.ns_bytes + p.part_bytes);
   }
-  if (a->rows == 0) return report_error(OSPREY_OK, "");
   Kv8AttnArgs k{};
   k.pool = pool_of(c);
   k.r = Kv8Rows{c->batch, a->rows, nullptr, a->cu_rows, a->cached, nullptr};

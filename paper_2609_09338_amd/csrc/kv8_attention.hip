@@ -66,7 +66,7 @@ __global__ void __launch_bounds__(256, (NT == 1 || !F32 ? 2 : 1)) k_kv8_attn(Kv8
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = blockIdx.x, group = a.nq / a.pool.nkv;
   const int n16 = lane & 15, qr = lane >> 4;
-  const Deal deal = deal_of(a, COLS, group, lane);
+  const Deal deal = deal_of(a, COLS, group, kUnit, lane);
   int at = deal.units ? blockIdx.y * deal.len : blockIdx.y;      // a unit, or an item
   const int at_end = deal.units ? min(at + deal.len, deal.units) : 0;
 

@@ -84,8 +84,8 @@ OSP_DEV int tiles_of(const Kv8Seq& s, int cols, int group) { return ((s.end - s.
 OSP_DEV int units_of(const Kv8Seq& s) { return (s.ctx + kUnit - 1) / kUnit; }
 
 // split_len: the caller's, or an even deal of the tiles' positions over the items that the launch
-// aims at, no finer than a unit and no more than n_split a sequence.
-OSP_DEV Deal deal_of(const Kv8AttnArgs& a, int cols, int group, int lane) {
+// aims at, no finer than the quantum (a unit) and no more than n_split a sequence.
+OSP_DEV Deal deal_of(const Kv8AttnArgs& a, int cols, int group, int quantum, int lane) {
   Deal d;
   d.mine = seq_or_none(a, lane);
   d.len = a.split_len;
@@ -102,6 +102,8 @@ OSP_DEV Deal deal_of(const Kv8AttnArgs& a, int cols, int group, int lane) {
   longest = wave_max_i(longest);
   if (a.by_units) {
     units = lane_i(wave_incl_scan<int>(units), 63);
+    d.len = kUnit;
+    if (units == 0) return d;   // no row, no item
     const int even = (units + a.items - 1) / a.items;
     // By splits where they come out even: a split a block, at most a quarter longer than the even deal
     // (a second piece costs a block about as much as two or three units).
@@ -129,7 +131,7 @@ OSP_DEV Deal deal_of(const Kv8AttnArgs& a, int cols, int group, int lane) {
   const float even = work / (float)a.items;
   d.len = even < 1.0e9f ? (int)even + 1 : 1000000000;
   d.len = max(d.len, (longest + a.n_split - 1) / a.n_split);
-  d.len = (d.len + kUnit - 1) / kUnit * kUnit;
+  d.len = (d.len + quantum - 1) / quantum * quantum;
   return d;
 }
 
@@ -171,7 +173,7 @@ OSP_DEV bool find_item(const Kv8AttnArgs& a, const Deal& d, int it, int cols, in
   int before = 0;
   for (int b0 = 0; b0 < a.r.B; b0 += 64) {
     const Kv8Seq s = b0 == 0 ? d.mine : seq_or_none(a, b0 + lane);
-    const int tiles = tiles_of(s, cols, group), ns = (s.ctx + d.len - 1) / d.len;
+    const int tiles = tiles_of(s, cols, group), ns = min((s.ctx + d.len - 1) / d.len, a.n_split);
     const int n = tiles * ns;
     const int incl = wave_incl_scan<int>(n);
     const uint64_t past = __builtin_amdgcn_ballot_w64(before + incl > it);

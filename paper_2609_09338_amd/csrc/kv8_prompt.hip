@@ -33,7 +33,7 @@ __global__ void __launch_bounds__(64 * NW, 2) k_kv8_prompt(Kv8AttnArgs a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = blockIdx.x, group = a.nq / a.pool.nkv;
   const int n16 = lane & 15, qr = lane >> 4;
-  const Deal deal = deal_of(a, COLS, group, lane);
+  const Deal deal = deal_of(a, COLS, group, 32 * PAIRS, lane);
 
   for (int it = blockIdx.y;; it += gridDim.y) {
     Item x;
@@ -63,6 +63,7 @@ __global__ void __launch_bounds__(64 * NW, 2) k_kv8_prompt(Kv8AttnArgs a) {
     }
     // (the block walks together: to the end of what any of its vectors sees)
     lim_lo = wave_min_i(lim_lo);
+    lim_hi = wave_max_i(lim_hi);
     const int last = min((x.tile + 1) * COLS, nvec) - 1;
     const int t_hi = a.tree ? x.s.ctx : min(x.s.ctx, a.r.cached ? x.s.first + last / group + 1 : max(a.r.pos[x.s.beg + last / group], 0) + 1);
 
@@ -172,6 +173,8 @@ __global__ void __launch_bounds__(64 * NW, 2) k_kv8_prompt(Kv8AttnArgs a) {
 #pragma unroll
       for (int pr = 0; pr < PAIRS; ++pr) {
         const int at = in_chunk + 2 * pr, t0 = p_lo + (s * PAIRS + pr) * 32;
+        if (pr == 0 && s + 1 < n_steps) request(s + 1, ((s + 1) * PAIRS * 2 & 63) == 0 ? id_next : id_now);
+        if (t0 >= lim_hi) continue;   // (none of this wavefront's vectors sees the pair, or it has none)
         const bool oka = lane_i(id_now, at) >= 0, okb = lane_i(id_now, at + 1) >= 0;
         const float ska = lane_f(sk_now, at), skb = lane_f(sk_now, at + 1);
         const bool whole = t0 + 32 <= min(lim_lo, p_hi) && oka && okb;
@@ -200,7 +203,6 @@ __global__ void __launch_bounds__(64 * NW, 2) k_kv8_prompt(Kv8AttnArgs a) {
             for (int nt = 0; nt < NT; ++nt) sc[nt][(i + j) / KC] = mfma(__builtin_bit_cast(bf16x8, fr[i / 4 & 1][j]), qf[nt][(i + j) % KC], sc[nt][(i + j) / KC]);
           __builtin_amdgcn_sched_barrier(0);
         }
-        if (pr == 0 && s + 1 < n_steps) request(s + 1, ((s + 1) * PAIRS * 2 & 63) == 0 ? id_next : id);
         const float fa = score_factor(ska, colc), fb = score_factor(skb, colc);
         float z[NT][8], top = -INFINITY;
 #pragma unroll

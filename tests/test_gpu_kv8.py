@@ -519,3 +519,72 @@ def test_calls_on_another_stream_and_twice_give_the_same_bits():
         bd().kv8_attention(cache, q, o, lens, w, stream=s, **args)
     torch.cuda.synchronize()
     assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+
+
+def test_pages_behind_four_gib_and_layers_of_a_pool():
+    """A pool of 4.6 GB whose last pages are used, through the strides of its second layer."""
+    nkv, hd, pages = 4, 64, 280000
+    codes = torch.empty((pages, 2, 2, nkv, 16 * hd), dtype=torch.uint8, device=DEV)
+    assert codes.numel() > 1 << 32
+    scales = torch.empty((pages, 2, nkv, 2), dtype=F32, device=DEV)
+    cached = [40, 7]
+    table = ints([[pages - 1 - 7 * i for i in range(5)], [pages - 3 - 5 * i for i in range(5)]])
+    cache = bd().Kv8Cache(codes[:, 1], scales[:, 1], table, hd)
+    fill(cache, [50, 67], gen_of(1))
+    used = table.flatten().long()
+    small = torch.zeros((10, 2, nkv, 16 * hd), dtype=torch.uint8, device=DEV)
+    small.copy_(codes[used, 1])
+    ref = R.Cache(torch.nan_to_num(small.view(torch.float8_e4m3fn).float(), nan=0.0).to(torch.float8_e4m3fn).view(torch.uint8),
+                  torch.nan_to_num(scales[used, 1], nan=1.0, posinf=1.0, neginf=1.0), torch.arange(10).view(2, 5), hd)
+    check_attention(cache, cached, [10, 60], BF, gen_of(2), 8, ref=ref)
+    check_attention(cache, [49, 66], [1, 1], F32, gen_of(2), 8, ref=ref)
+
+
+def test_calls_with_nothing_to_do_leave_everything_as_it_was():
+    nkv, hd = 2, 64
+    cache = make_cache(2, 3, nkv, hd, 4)
+    fill(cache, [20, 5], gen_of(1))
+    before = (cache.codes.clone(), cache.scales.clone())
+    none = torch.empty((0, nkv, hd), device=DEV)
+    bd().kv8_append(cache, none, none, ints([20, 5]), q=none, q_out=none, cu_rows=ints([0, 0, 0]))
+    some = torch.randn((3, nkv, hd), generator=gen_of(1), device=DEV)
+    out = torch.full((3, nkv, hd), 7.0, device=DEV)
+    bd().kv8_append(cache, some, some, ints([20, 5]), q=some, q_out=out, cu_rows=ints([0, 0, 0]))   # rows behind the last sequence
+    ws = torch.empty(bd().kv8_attention_workspace(cache, 3, nkv, 1, 300), dtype=torch.uint8, device=DEV)
+    bd().kv8_attention(cache, none, none, ints([20, 5]), ws, cu_rows=ints([0, 0, 0]))
+    for context in (1, 300):
+        bd().kv8_attention(cache, some, out, ints([20, 5]), ws, max_context=context, cu_rows=ints([0, 0, 0]))
+    bd().kv8_keep(cache, ints([20, 5]), ints([[0], [0]]), ints([0, -3]))
+    torch.cuda.synchronize()
+    assert bool((out == 7.0).all())
+    assert torch.equal(cache.codes, before[0]) and torch.equal(cache.scales.nan_to_num(), before[1].nan_to_num())
+
+
+@pytest.mark.parametrize("dtype,rows", [(BF, 4), (F32, 4), (BF, 70)])
+def test_a_query_that_is_not_finite_spoils_its_own_row_only(dtype, rows):
+    nq, nkv, hd = 4, 2, 64
+    cache = make_cache(1, 20, nkv, hd, 4)
+    fill(cache, [300], gen_of(1))
+    q = torch.randn((rows, nq, hd), generator=gen_of(2), device=DEV).to(dtype)
+    ws = torch.empty(bd().kv8_attention_workspace(cache, rows, nq, rows, 300), dtype=torch.uint8, device=DEV)
+    outs = []
+    for spoil in (False, True):
+        if spoil:
+            q[1, 0, 3] = math.inf
+            q[2, 3, 9] = math.nan
+        out = torch.zeros_like(q)
+        bd().kv8_attention(cache, q, out, ints([300 - rows]), ws, max_rows=rows, max_context=300, cu_rows=ints([0, rows]))
+        outs.append(out.clone())
+    bad = torch.zeros((rows, nq), dtype=torch.bool, device=DEV)
+    bad[1, 0] = bad[2, 3] = True
+    assert torch.equal(outs[0][~bad], outs[1][~bad])
+    assert not bool(torch.isfinite(outs[1][bad]).all(-1).any())
+
+
+def test_long_context_among_short_ones_and_many_sequences():
+    """130 sequences, one of 9000 positions: splits by units, several deals of 64 sequences."""
+    cached = [9000] + [3 + 2 * b for b in range(129)]
+    cache = make_cache(130, 564, 2, 64, 7)
+    fill(cache, [c + 1 for c in cached], gen_of(3))
+    check_attention(cache, cached, [1] * 130, BF, gen_of(4), 4)
+    check_attention(cache, cached, [1] * 130, F32, gen_of(4), 2)
