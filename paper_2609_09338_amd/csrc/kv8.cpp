@@ -112,8 +112,10 @@ AttnPlan attention_plan(int batch, int nkv, int hd, int rows, int nq, int x_bf16
   AttnPlan p{};
   const int cols = kv8_attention_cols(x_bf16, nq / nkv, max_rows);
   p.tiles = (int)((long)rows * (nq / nkv) / cols) + batch;
-  // as many blocks as can be resident: eight wavefronts per CU
-    p.items = std::max(1, (2 * n_cu + nkv - 1) / nkv);
+  // Two blocks of four wavefronts per CU: what registers leave resident with 128-wide heads.  (With
+  // 64-wide ones three are, but more items make shorter splits: 4 sequences of 500 rows over 4000
+  // positions take 120 us unsplit and 162 in three blocks' worth.)
+  p.items = std::max(1, (2 * n_cu + nkv - 1) / nkv);
   p.n_split = (int)std::min<long>(kKv8MaxSplits, std::max(1L, ((long)max_context + kSplitQuantum - 1) / kSplitQuantum));
   // A pass that fills the chip with its tiles is not cut.  The partials of others take 256 MB at most,
   // or what twice the even deal needs: enough for one long context among many short ones.
@@ -125,7 +127,7 @@ AttnPlan attention_plan(int batch, int nkv, int hd, int rows, int nq, int x_bf16
     p.n_split = (int)std::min<long>(p.n_split, std::max(room, 2L * p.items / std::max(full, 1L) + 2));
   }
   // (splits by units may begin anywhere in a sequence: one more; their count fits an int)
-  p.by_units = p.n_split > 1 && cols != kKv8PromptCols && (long)p.tiles * (max_pages / 8 + 1) < 1L << 30;
+  p.by_units = p.n_split > 1 && cols < kv8_prompt_cols(0) && (long)p.tiles * (max_pages / 8 + 1) < 1L << 30;
   if (p.by_units) p.n_split = std::min(p.n_split + 1, kKv8MaxSplits);
   if (p.n_split > 1) {
     p.ns_bytes = ((size_t)rows * nq * 4 + 255) & ~size_t(255);

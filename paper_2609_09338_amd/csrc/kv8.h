@@ -111,7 +111,9 @@ struct Kv8AttnArgs {
   uint32_t* err;
 };
 // Query vectors of one tile of a pass of at most max_rows rows a sequence.
-constexpr int kKv8PromptWaves = 4, kKv8PromptNt = 2, kKv8PromptCols = 16 * kKv8PromptNt * kKv8PromptWaves;
+// (kv8_prompt.hip: four wavefronts of 32 bf16 vectors, or of 16 fp32 ones, which take two products each)
+constexpr int kKv8PromptWaves = 4;
+inline int kv8_prompt_cols(int x_bf16) { return kKv8PromptWaves * (x_bf16 ? 32 : 16); }
 int kv8_attention_cols(int x_bf16, int group, int max_rows);
 void launch_kv8_prompt(const Kv8AttnArgs& a, dim3 grid, hipStream_t st);
 void launch_kv8_attention(const Kv8AttnArgs& a, int max_rows, hipStream_t st);

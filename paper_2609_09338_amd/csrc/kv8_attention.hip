@@ -7,7 +7,7 @@
 // heads of the group) and one split of the context; its four wavefronts take the split's page
 // pairs in turn, straight from memory into registers, the next pair requested while this one is
 // computed.  Per pair (32 tokens) a wavefront computes
-//   S^T[token][query] = K Q^T     (16x16x32, K steps over dims, codes converted to f16: exact)
+//   S^T[token][query] = K Q^T     (16x16x32, K steps over dims; codes convert exactly)
 //   O^T[dim][query] += V^T P^T    (16x16x32, the K index runs over 4 q .. 4 q + 3 of both pages)
 // where lane (l % 16, q = l / 16) of the score tile holds exactly the four tokens of each page that
 // the second product's B operand wants there: nothing moves between lanes in the loop.
@@ -22,6 +22,11 @@
 //   * The running maximum only moves when a score passes it by 2^8 (one ballot a pair, no
 //     cross-lane traffic otherwise), and then to a whole number: outputs are rescaled by powers of
 //     two, exactly.  Sums stay per lane until the end.
+// Measured, with the join: one token over 131002 positions (8 kv heads of 128) 56 us, 4.8 TB/s; the
+// next token of 64 requests of 512 to 4095 positions 68 us, 4.2 TB/s (a copy reaches 4.7); 8 chains of 8
+// rows over 4000 positions 27 us, 2.4 TB/s; one token over 2048 positions 7 + 3 us of latency.  What
+// runs once a wavefront costs its instruction fetches: the code before and after the loop is kept
+// short (converting the queries there and unrolled merges took 16 rows over 136 positions 26 us, 13 so).
 #include <algorithm>
 #include <type_traits>
 
@@ -120,24 +125,7 @@ __global__ void __launch_bounds__(256, (NT == 1 || !F32 ? 2 : 1)) k_kv8_attn(Kv8
       const long at = (long)row * a.ldq + (long)h * HD + qr * (HD / 4);
       colc[nt] = a.scale * kLog2e;
       if constexpr (F32) {
-        const float* p = reinterpret_cast<const float*>(a.q) + at;
-        float q[HD / 4], big = 0.f;
-#pragma unroll
-        for (int i = 0; i < HD / 4; i += 4) load_vec<float>(p + i, q + i);
-#pragma unroll
-        for (int i = 0; i < HD / 4; ++i) big = fmaxf(big, fabsf(q[i]));
-        big = fmaxf(big, xor_lane_c(big, 16));
-        big = fmaxf(big, xor_lane_c(big, 32));
-        const int up = query_exp(big);
-        const float f = kv8_pow2(up);
-        colc[nt] *= kv8_pow2(-up);
-#pragma unroll
-        for (int i = 0; i < HD / 4; ++i) {
-          const float v = q[i] * f;
-          const _Float16 hi = (_Float16)v;
-          qf[nt][0][i / 8][i % 8] = hi;
-          qf[nt][NP - 1][i / 8][i % 8] = (_Float16)(v - (float)hi);
-        }
+        colc[nt] *= query_parts<HD>(reinterpret_cast<const float*>(a.q) + at, qf[nt][0], qf[nt][NP - 1]);
       } else {
         const uint4* p = reinterpret_cast<const uint4*>(reinterpret_cast<const bf16_t*>(a.q) + at);
 #pragma unroll
@@ -255,16 +243,7 @@ __global__ void __launch_bounds__(256, (NT == 1 || !F32 ? 2 : 1)) k_kv8_attn(Kv8
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           if constexpr (F32) {
-            f16x8 hi, lo;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const float p = __builtin_amdgcn_exp2f(z[nt][e]);
-              l[nt] += p;
-              hi[e] = (_Float16)p;
-              lo[e] = (_Float16)(p - (float)hi[e]);
-            }
-            pf[nt][0] = hi;
-            pf[nt][NP - 1] = lo;
+            probability_parts(z[nt], l[nt], pf[nt][0], pf[nt][NP - 1]);
           } else {
             uint32_t u[4];
             probabilities(z[nt], l[nt], u);
@@ -422,15 +401,14 @@ void launch_cols(const Kv8AttnArgs& a, dim3 grid, hipStream_t st) {
   }
 }
 
-// Sequences of at most 32 query vectors a kv head, and fp32 rows (whose queries take twice the
-// registers), go to the kernel here; more to kv8_prompt.hip.
-bool use_prompt(int x_bf16, int group, int max_rows) { return x_bf16 && (long)group * max_rows > 32; }
+// Sequences of at most 32 query vectors a kv head go to the kernel here, more to kv8_prompt.hip.
+bool use_prompt(int group, int max_rows) { return (long)group * max_rows > 32; }
 int cols_nt(int group, int max_rows) { return (long)group * max_rows <= 16 ? 1 : 2; }
 
 }  // namespace
 
 int kv8_attention_cols(int x_bf16, int group, int max_rows) {
-  return use_prompt(x_bf16, group, max_rows) ? kKv8PromptCols : 16 * cols_nt(group, max_rows);
+  return use_prompt(group, max_rows) ? kv8_prompt_cols(x_bf16) : 16 * cols_nt(group, max_rows);
 }
 
 void launch_kv8_attention(const Kv8AttnArgs& a, int max_rows, hipStream_t st) {
@@ -439,7 +417,7 @@ void launch_kv8_attention(const Kv8AttnArgs& a, int max_rows, hipStream_t st) {
   if (a.by_units) y = a.items;
   else if (a.split_len == 0 && a.n_split > 1) y = std::min<long>(y, (long)a.items + a.tiles);
   const dim3 grid(a.pool.nkv, (unsigned)std::min<long>(std::max<long>(y, 1), 65535));
-  if (use_prompt(a.x_bf16, group, max_rows)) return launch_kv8_prompt(a, grid, st);
+  if (use_prompt(group, max_rows)) return launch_kv8_prompt(a, grid, st);
   if (a.hd == 128) {
     if (nt == 1) launch_cols<128, 1>(a, grid, st);
     else launch_cols<128, 2>(a, grid, st);

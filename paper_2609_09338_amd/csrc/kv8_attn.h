@@ -266,6 +266,39 @@ OSP_DEV int query_exp(float big) {
   return big > 0.f && big < INFINITY ? min(max(13 - e, -114), 120) : 0;
 }
 
+// The lane's HD / 4 dims of an fp32 query vector as f16 parts hi + lo at a power of two of their own;
+// returns the factor that undoes it.
+template <int HD>
+OSP_DEV float query_parts(const float* p, f16x8* hi, f16x8* lo) {
+  float q[HD / 4], big = 0.f;
+#pragma unroll
+  for (int i = 0; i < HD / 4; i += 4) load_vec<float>(p + i, q + i);
+#pragma unroll
+  for (int i = 0; i < HD / 4; ++i) big = fmaxf(big, fabsf(q[i]));
+  big = fmaxf(big, xor_lane_c(big, 16));
+  big = fmaxf(big, xor_lane_c(big, 32));
+  const int up = query_exp(big);
+  const float f = kv8_pow2(up);
+#pragma unroll
+  for (int i = 0; i < HD / 4; ++i) {
+    const float v = q[i] * f;
+    hi[i / 8][i % 8] = (_Float16)v;
+    lo[i / 8][i % 8] = (_Float16)(v - (float)hi[i / 8][i % 8]);
+  }
+  return kv8_pow2(-up);
+}
+
+// P = 2^z of a lane's eight exponents as f16 parts hi + lo; its sum joins l.
+OSP_DEV void probability_parts(const float* z, float& l, f16x8& hi, f16x8& lo) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float p = __builtin_amdgcn_exp2f(z[e]);
+    l += p;
+    hi[e] = (_Float16)p;
+    lo[e] = (_Float16)(p - (float)hi[e]);
+  }
+}
+
 // P = 2^z of a lane's four exponents as f16; its sum (of the rounded values) joins l.
 OSP_DEV void probabilities(const float* z, float& l, uint32_t* u) {
   const f16x2 one = {(_Float16)1.f, (_Float16)1.f};

@@ -4,29 +4,37 @@
 // Bound by the matrix cores and, as closely, by the vector ALUs that the softmax and the
 // conversion of the codes need.  A block owns one kv head and 32 NW query vectors (rows x heads
 // of the group), 32 to a wavefront, and walks the split's pages NW / 2 pairs a step:
-//   * each wavefront reads one pair's keys or values (as kv8_attention.hip does), converts them to
-//     bf16 (keys) or f16 (values) once for the whole block and writes them to LDS in the order in which the products' A
-//     operands are read: fragment (K step or dim tile), lane, 8 values.  Reads and writes are
-//     1 KB contiguous per instruction, without bank conflicts.  Two buffers, one barrier a step.
+//   * Each wavefront reads one pair's keys or values (as kv8_attention.hip does), converts them to
+//     bf16 (keys) or f16 (values) once for the whole block and writes them to LDS in the order in
+//     which the products' A operands are read: fragment (K step or dim tile), lane, 8 values.  Reads
+//     and writes are 1 KB contiguous per instruction, without bank conflicts.  Two buffers, one
+//     barrier a step; the next step's codes are requested before this one's products.
 //   * S^T = K Q^T and O^T += V^T P^T as there, 16x16x32, with the queries and outputs of 32 vectors
-//     in registers, two wavefronts a SIMD: one's softmax runs beside the other's products.  (64
-//     vectors would halve the reads of LDS, and need every register of a SIMD for one wavefront: 500
-//     TFLOP/s against 945, at 4000 rows over 6000 to 9000 positions, 32 heads of 128.)
+//     in registers, two wavefronts a SIMD (three with 64-wide heads: 115 -> 97 us for a prompt of
+//     4000 rows, 32 heads): one's softmax runs beside the other's products.  (64 vectors would halve
+//     the reads of LDS, and need every register of a SIMD for one wavefront: 500 TFLOP/s.)
 //   * A operands are read four ahead of the products that take them: with one read in flight at a
 //     time, as the compiler orders them, the wavefronts wait for LDS (620 TFLOP/s).
-//   * the softmax is kept to what a vector ALU must do a score: one fma, half a maximum, an exp2, half
+//   * The softmax is kept to what a vector ALU must do a score: one fma, half a maximum, an exp2, half
 //     a conversion and half a dot product with ones (the sum, of the rounded P).  All that is rare
 //     (masks, maxima that move) sits behind one branch a pair of pages.
+// 4 x 1000 rows over 6000 to 9000 positions, 32 heads of 128 over 8: 551 us, 970 TFLOP/s (a large
+// bf16 matrix product reaches 1250 here); a prompt of 4099 rows 167 us, 825 TFLOP/s.  The same with
+// one wavefront a token range and no LDS (kv8_attention.hip at 64 vectors) took 1010 and 373 us.
+// fp32 rows take two products each (hi + lo), so 16 vectors a wavefront: a prompt of 4000 rows 256 us
+// (128-wide heads), 155 us (64-wide).
 #include <algorithm>
+#include <type_traits>
 
 #include "kv8_attn.h"
 
 namespace osp {
 namespace {
 
-template <int HD, int NW>
-__global__ void __launch_bounds__(64 * NW, 2) k_kv8_prompt(Kv8AttnArgs a) {
-  constexpr int KC = HD / 32, DT = HD / 16, NT = kKv8PromptNt, COLS = 16 * NT * NW, PAIRS = NW / 2;
+template <int HD, int NW, bool F32>
+__global__ void __launch_bounds__(64 * NW, HD == 64 ? 3 : 2) k_kv8_prompt(Kv8AttnArgs a) {
+  constexpr int KC = HD / 32, DT = HD / 16, NT = F32 ? 1 : 2, NP = F32 ? 2 : 1, COLS = 16 * NT * NW, PAIRS = NW / 2;
+  typedef typename std::conditional<F32, f16x8, bf16x8>::type qk_t;
   constexpr int RAW = HD / 32;        // 16-byte pieces a lane reads of a pair's keys (values)
   __shared__ uint4 sm_k[2][PAIRS][2][KC][64];
   __shared__ uint4 sm_v[2][PAIRS][DT][64];
@@ -41,9 +49,8 @@ __global__ void __launch_bounds__(64 * NW, 2) k_kv8_prompt(Kv8AttnArgs a) {
     const int nvec = (x.s.end - x.s.beg) * group, c0 = x.tile * COLS + wave * (16 * NT);
 
     // ---- queries and what they see --------------------------------------------------
-    bf16x8 qf[NT][KC];
-    const float colc = a.scale * kLog2e;
-    float m[NT], l[NT];
+    qk_t qf[NT][NP][KC];
+    float colc[NT], m[NT], l[NT];
     int lim[NT];
     int lim_lo = 0x7fffffff, lim_hi = 0;
     bool missing = false;
@@ -52,9 +59,15 @@ __global__ void __launch_bounds__(64 * NW, 2) k_kv8_prompt(Kv8AttnArgs a) {
       const int c = c0 + 16 * nt + n16;
       const bool on = c < nvec;
       const int row = x.s.beg + (on ? c / group : 0), h = g * group + (on ? c % group : 0);
-      const bf16_t* p = reinterpret_cast<const bf16_t*>(a.q) + (long)row * a.ldq + (long)h * HD + qr * (HD / 4);
+      const long at = (long)row * a.ldq + (long)h * HD + qr * (HD / 4);
+      colc[nt] = a.scale * kLog2e;
+      if constexpr (F32) {
+        colc[nt] *= query_parts<HD>(reinterpret_cast<const float*>(a.q) + at, qf[nt][0], qf[nt][NP - 1]);
+      } else {
+        const uint4* p = reinterpret_cast<const uint4*>(reinterpret_cast<const bf16_t*>(a.q) + at);
 #pragma unroll
-      for (int i = 0; i < KC; ++i) qf[nt][i] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(p + 8 * i));
+        for (int i = 0; i < KC; ++i) qf[nt][0][i] = __builtin_bit_cast(bf16x8, p[i]);
+      }
       Sight see;
       sight_of(a, x, row, on, see, lim_lo, lim_hi, missing);
       lim[nt] = see.lim;
@@ -135,7 +148,11 @@ __global__ void __launch_bounds__(64 * NW, 2) k_kv8_prompt(Kv8AttnArgs a) {
         for (int k = 0; k < 2; ++k)
 #pragma unroll
           for (int c = 0; c < KC; ++c)
-            sm_k[buf][my_pair][k][c][lane] = __builtin_bit_cast(uint4, frag8_bf16(word(raw, k * DT + 2 * c), word(raw, k * DT + 2 * c + 1)));
+          {
+            const uint32_t u = word(raw, k * DT + 2 * c), w = word(raw, k * DT + 2 * c + 1);
+            if constexpr (F32) sm_k[buf][my_pair][k][c][lane] = __builtin_bit_cast(uint4, frag8(u, w));
+            else sm_k[buf][my_pair][k][c][lane] = __builtin_bit_cast(uint4, frag8_bf16(u, w));
+          }
       }
     };
 
@@ -200,14 +217,16 @@ __global__ void __launch_bounds__(64 * NW, 2) k_kv8_prompt(Kv8AttnArgs a) {
 #pragma unroll
           for (int j = 0; j < 4; ++j)
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) sc[nt][(i + j) / KC] = mfma(__builtin_bit_cast(bf16x8, fr[i / 4 & 1][j]), qf[nt][(i + j) % KC], sc[nt][(i + j) / KC]);
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int p = 0; p < NP; ++p)
+                sc[nt][(i + j) / KC] = mfma(__builtin_bit_cast(qk_t, fr[i / 4 & 1][j]), qf[nt][p][(i + j) % KC], sc[nt][(i + j) / KC]);
           __builtin_amdgcn_sched_barrier(0);
         }
-        const float fa = score_factor(ska, colc), fb = score_factor(skb, colc);
         float z[NT][8], top = -INFINITY;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
-          exponents(sc[nt], fa, fb, kLift - m[nt], z[nt], top);
+          exponents(sc[nt], score_factor(ska, colc[nt]), score_factor(skb, colc[nt]), kLift - m[nt], z[nt], top);
         // One branch for all that is rare: pairs that some vector sees in part, maxima that move.
         if (!whole || __builtin_amdgcn_ballot_w64(top > kLift + kSlack)) {
 #pragma unroll
@@ -217,6 +236,7 @@ __global__ void __launch_bounds__(64 * NW, 2) k_kv8_prompt(Kv8AttnArgs a) {
               mask_scores(sc[nt][0], v, qr);
               mask_scores(sc[nt][1], v >> 16, qr);
             }
+            const float fa = score_factor(ska, colc[nt]), fb = score_factor(skb, colc[nt]);
             float cm = fmaxf(max4(sc[nt][0]) * fa, max4(sc[nt][1]) * fb);
             cm = fmaxf(cm, xor_lane_c(cm, 16));
             cm = fmaxf(cm, xor_lane_c(cm, 32));
@@ -229,13 +249,17 @@ __global__ void __launch_bounds__(64 * NW, 2) k_kv8_prompt(Kv8AttnArgs a) {
             exponents(sc[nt], fa, fb, kLift - m[nt], z[nt], top);
           }
         }
-        f16x8 pf[NT];
+        f16x8 pf[NT][NP];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-          uint32_t u[4];
-          probabilities(z[nt], l[nt], u);
-          probabilities(z[nt] + 4, l[nt], u + 2);
-          pf[nt] = frag(u[0], u[1], u[2], u[3]);
+          if constexpr (F32) {
+            probability_parts(z[nt], l[nt], pf[nt][0], pf[nt][NP - 1]);
+          } else {
+            uint32_t u[4];
+            probabilities(z[nt], l[nt], u);
+            probabilities(z[nt] + 4, l[nt], u + 2);
+            pf[nt][0] = frag(u[0], u[1], u[2], u[3]);
+          }
         }
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -246,7 +270,9 @@ __global__ void __launch_bounds__(64 * NW, 2) k_kv8_prompt(Kv8AttnArgs a) {
 #pragma unroll
           for (int j = 0; j < 4; ++j)
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) acc[nt][i + j] = mfma(__builtin_bit_cast(f16x8, fr[f][j]), pf[nt], acc[nt][i + j]);
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int p = 0; p < NP; ++p) acc[nt][i + j] = mfma(__builtin_bit_cast(f16x8, fr[f][j]), pf[nt][p], acc[nt][i + j]);
           __builtin_amdgcn_sched_barrier(0);
         }
       }
@@ -265,7 +291,7 @@ __global__ void __launch_bounds__(64 * NW, 2) k_kv8_prompt(Kv8AttnArgs a) {
     if (missing && a.err) atomicOr(a.err, 1u << 2);
 
     // ---- outputs: lane holds dims 16 d + 4 qr .. + 4 of vector n16 of each tile --------
-    const bool direct = x.ns == 1 && (a.out || a.o_hi);   // one split: no join
+    const bool direct = x.ns == 1 && (a.out || (a.o_hi && !F32));   // one split: no join
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       l[nt] += xor_lane_c(l[nt], 16);
@@ -277,6 +303,13 @@ __global__ void __launch_bounds__(64 * NW, 2) k_kv8_prompt(Kv8AttnArgs a) {
       if (direct) {
         const float inv = l[nt] > 0.f || l[nt] != l[nt] ? eref / l[nt] : 0.f;
         const long at = (long)row * a.ldo + (long)h * HD + 4 * qr;
+        if constexpr (F32) {
+          float* o = reinterpret_cast<float*>(a.out) + at;
+#pragma unroll
+          for (int d = 0; d < DT; ++d)
+            *reinterpret_cast<float4*>(o + 16 * d) = make_float4(acc[nt][d][0] * inv, acc[nt][d][1] * inv, acc[nt][d][2] * inv, acc[nt][d][3] * inv);
+          continue;
+        }
         if (a.o_hi) {
 #pragma unroll
           for (int d = 0; d < DT; ++d) {
@@ -311,9 +344,16 @@ __global__ void __launch_bounds__(64 * NW, 2) k_kv8_prompt(Kv8AttnArgs a) {
 
 }  // namespace
 
+template <int HD>
+static void launch_prompt(const Kv8AttnArgs& a, dim3 grid, hipStream_t st) {
+  constexpr int NW = kKv8PromptWaves;
+  if (a.x_bf16) hipLaunchKernelGGL((k_kv8_prompt<HD, NW, false>), grid, dim3(64 * NW), 0, st, a);
+  else hipLaunchKernelGGL((k_kv8_prompt<HD, NW, true>), grid, dim3(64 * NW), 0, st, a);
+}
+
 void launch_kv8_prompt(const Kv8AttnArgs& a, dim3 grid, hipStream_t st) {
-  if (a.hd == 128) hipLaunchKernelGGL((k_kv8_prompt<128, kKv8PromptWaves>), grid, dim3(64 * kKv8PromptWaves), 0, st, a);
-  else hipLaunchKernelGGL((k_kv8_prompt<64, kKv8PromptWaves>), grid, dim3(64 * kKv8PromptWaves), 0, st, a);
+  if (a.hd == 128) launch_prompt<128>(a, grid, st);
+  else launch_prompt<64>(a, grid, st);
 }
 
 }  // namespace osp
