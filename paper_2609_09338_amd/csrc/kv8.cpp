@@ -104,18 +104,19 @@ constexpr int kSplitQuantum = 128;
 constexpr long kPartBytes = 256L << 20;
 
 struct AttnPlan {
-  int n_split, tiles, items, by_units;
+  int form, n_split, tiles, items, by_units;
   size_t ns_bytes, part_bytes;
 };
 AttnPlan attention_plan(int batch, int nkv, int hd, int rows, int nq, int x_bf16, int max_rows, int max_context, int max_pages,
                         int n_cu) {
   AttnPlan p{};
-  const int cols = kv8_attention_cols(x_bf16, nq / nkv, max_rows);
+  p.form = kv8_attention_form(x_bf16, nq / nkv, max_rows, (long)batch * max_context, nkv);
+  const int cols = kv8_form_cols(p.form, x_bf16);
   p.tiles = (int)((long)rows * (nq / nkv) / cols) + batch;
-  // Two blocks of four wavefronts per CU: what registers leave resident with 128-wide heads.  (With
-  // 64-wide ones three are, but more items make shorter splits: 4 sequences of 500 rows over 4000
-  // positions take 120 us unsplit and 162 in three blocks' worth.)
-  p.items = std::max(1, (2 * n_cu + nkv - 1) / nkv);
+  // Eight wavefronts per CU: what registers leave resident with 128-wide heads.  (With 64-wide ones
+  // twelve are, but more items make shorter splits: 4 sequences of 500 rows over 4000 positions take
+  // 120 us unsplit and 162 in three blocks' worth.)
+  p.items = std::max(1, ((p.form == kKv8Shared ? 1 : 2) * n_cu + nkv - 1) / nkv);
   p.n_split = (int)std::min<long>(kKv8MaxSplits, std::max(1L, ((long)max_context + kSplitQuantum - 1) / kSplitQuantum));
   // A pass that fills the chip with its tiles is not cut.  The partials of others take 256 MB at most,
   // or what twice the even deal needs: enough for one long context among many short ones.
@@ -127,7 +128,7 @@ AttnPlan attention_plan(int batch, int nkv, int hd, int rows, int nq, int x_bf16
     p.n_split = (int)std::min<long>(p.n_split, std::max(room, 2L * p.items / std::max(full, 1L) + 2));
   }
   // (splits by units may begin anywhere in a sequence: one more; their count fits an int)
-  p.by_units = p.n_split > 1 && cols < kv8_prompt_cols(0) && (long)p.tiles * (max_pages / 8 + 1) < 1L << 30;
+  p.by_units = p.n_split > 1 && p.form != kKv8Prompt && (long)p.tiles * (max_pages / 8 + 1) < 1L << 30;
   if (p.by_units) p.n_split = std::min(p.n_split + 1, kKv8MaxSplits);
   if (p.n_split > 1) {
     p.ns_bytes = ((size_t)rows * nq * 4 + 255) & ~size_t(255);
@@ -242,6 +243,7 @@ OSPREY_API int osprey_kv8_attention(const osprey_kv8_cache* c, const osprey_kv8_
   k.hd = c->head_dim;
   k.scale = a->scale;
   k.tree = a->tree_mask;
+  k.form = p.form;
   k.n_split = p.n_split;
   k.items = p.items;
   k.by_units = p.by_units;
@@ -255,7 +257,7 @@ OSPREY_API int osprey_kv8_attention(const osprey_kv8_cache* c, const osprey_kv8_
     k.row_ns = (int32_t*)a->workspace;
     k.part = (float*)((char*)a->workspace + p.ns_bytes);
   }
-  launch_kv8_attention(k, a->max_rows, (hipStream_t)hip_stream);
+  launch_kv8_attention(k, (hipStream_t)hip_stream);
   if (p.n_split > 1) launch_kv8_join(k, (hipStream_t)hip_stream);
   return done();
 }

@@ -96,6 +96,7 @@ struct Kv8AttnArgs {
   int nq, hd;
   float scale;
   const uint64_t* tree;     // [rows][2] bit i: the row sees position cached + i (nullable: causal)
+  int form;                 // kKv8Narrow ..
   int n_split;              // partials per row and head
   int split_len;            // positions per split (0: planned on the device from the lengths)
   int by_units;             // the work is dealt by units of positions across sequences (kv8_attn.h)
@@ -110,13 +111,17 @@ struct Kv8AttnArgs {
   uint16_t *o_hi, *o_lo;    // or bf16 pairs [rows][nq hd] (kv8_prompt.hip, one split; nullable)
   uint32_t* err;
 };
-// Query vectors of one tile of a pass of at most max_rows rows a sequence.
+// The kernel of a pass of at most max_rows rows a sequence whose contexts are `positions` in all, and
+// the query vectors of one of its tiles.
+enum { kKv8Narrow = 0, kKv8Shared = 1, kKv8Both = 2, kKv8Prompt = 3 };
+int kv8_attention_form(int x_bf16, int group, int max_rows, long positions, int nkv);
 // (kv8_prompt.hip: four wavefronts of 32 bf16 vectors, or of 16 fp32 ones, which take two products each)
 constexpr int kKv8PromptWaves = 4;
-inline int kv8_prompt_cols(int x_bf16) { return kKv8PromptWaves * (x_bf16 ? 32 : 16); }
-int kv8_attention_cols(int x_bf16, int group, int max_rows);
+inline int kv8_form_cols(int form, int x_bf16) {
+  return form == kKv8Narrow ? 16 : form != kKv8Prompt ? 32 : kKv8PromptWaves * (x_bf16 ? 32 : 16);
+}
 void launch_kv8_prompt(const Kv8AttnArgs& a, dim3 grid, hipStream_t st);
-void launch_kv8_attention(const Kv8AttnArgs& a, int max_rows, hipStream_t st);
+void launch_kv8_attention(const Kv8AttnArgs& a, hipStream_t st);
 // out = the splits' joined outputs (a.n_split > 1)
 void launch_kv8_join(const Kv8AttnArgs& a, hipStream_t st);
 

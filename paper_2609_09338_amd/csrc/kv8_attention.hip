@@ -3,10 +3,11 @@
 //
 //   o_r = sum_t softmax_t(scale q_r . k_t) v_t over the positions t that row r sees
 //
-// Bound by the codes' bytes.  A block owns one kv head, one tile of 16 NT query vectors (rows x
-// heads of the group) and one split of the context; its four wavefronts take the split's page
-// pairs in turn, straight from memory into registers, the next pair requested while this one is
-// computed.  Per pair (32 tokens) a wavefront computes
+// Bound by the codes' bytes.  A block owns one kv head, one tile of 16 NT CT query vectors (rows x
+// heads of the group) and one split of the context; its four wavefronts (CT = 2: twice four, each
+// four for half of the vectors) take the split's page pairs in turn, straight from memory into
+// registers, the next pair requested while this one is computed.  Per pair (32 tokens) a wavefront
+// computes
 //   S^T[token][query] = K Q^T     (16x16x32, K steps over dims; codes convert exactly)
 //   O^T[dim][query] += V^T P^T    (16x16x32, the K index runs over 4 q .. 4 q + 3 of both pages)
 // where lane (l % 16, q = l / 16) of the score tile holds exactly the four tokens of each page that
@@ -24,7 +25,7 @@
 //     two, exactly.  Sums stay per lane until the end.
 // Measured, with the join: one token over 131002 positions (8 kv heads of 128) 56 us, 4.8 TB/s; the
 // next token of 64 requests of 512 to 4095 positions 68 us, 4.2 TB/s (a copy reaches 4.7); 8 chains of 8
-// rows over 4000 positions 27 us, 2.4 TB/s; one token over 2048 positions 7 + 3 us of latency.  What
+// rows over 4000 positions 25.5 us, 2.6 TB/s; one token over 2048 positions 7 + 3 us of latency.  What
 // runs once a wavefront costs its instruction fetches: the code before and after the loop is kept
 // short (converting the queries there and unrolled merges took 16 rows over 136 positions 26 us, 13 so).
 #include <algorithm>
@@ -59,16 +60,17 @@ template <int HD> struct Page {
   OSP_DEV uint32_t vd(int i) const { return word(v, i); }
 };
 
-template <int HD, int NT, bool F32, bool STREAM>
-__global__ void __launch_bounds__(256, (NT == 1 || !F32 ? 2 : 1)) k_kv8_attn(Kv8AttnArgs a) {
+template <int HD, int NT, int CT, bool F32, bool STREAM>
+__global__ void __launch_bounds__(256 * CT, NT == 1 || !F32 ? 2 : 1) k_kv8_attn(Kv8AttnArgs a) {
   constexpr int KC = HD / 32;         // K steps of the score product
   constexpr int DT = HD / 16;         // 16-row tiles of dims
   constexpr int NP = F32 ? 2 : 1;     // parts of Q and P
   constexpr int DEPTH = 2;            // pairs in registers
-  constexpr int COLS = 16 * NT;
+  constexpr int COLS = 16 * NT * CT;
   __shared__ float sm_o[4][COLS][HD + 4];
   __shared__ float sm_m[4][COLS], sm_l[4][COLS];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, w8 = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wave = w8 & 3, v0 = (w8 >> 2) * 16 * NT;   // its share of the pages, its first vector
   const int g = blockIdx.x, group = a.nq / a.pool.nkv;
   const int n16 = lane & 15, qr = lane >> 4;
   const Deal deal = deal_of(a, COLS, group, kUnit, lane);
@@ -94,9 +96,11 @@ __global__ void __launch_bounds__(256, (NT == 1 || !F32 ? 2 : 1)) k_kv8_attn(Kv8
     const long k_off = (long)g * (kKv8Page * HD) + n16 * HD + qr * (HD / 4);
     const long v_off = (long)(a.pool.nkv + g) * (kKv8Page * HD) + qr * 4 * HD + n16 * (HD / 4);
     // 32 of the wavefront's pairs at a time, a page a lane (-1: none, -2: not in the split)
+    const int n_pairs = (s_hi - p_lo + 31) / 32, mine = n_pairs > wave ? (n_pairs - wave + 3) / 4 : 0;
+    auto pair_at = [&](int i) { return p_lo + (wave + 4 * i) * 32; };
     auto pages_at = [&](int i0) {
-      const int t = p_lo + (wave + 4 * (i0 + (lane >> 1))) * 32 + (lane & 1) * 16;
-      return t < s_hi ? kv8_page(a.pool, x.b, t / kKv8Page) : -2;
+      const int i = lane >> 1, t = pair_at(i0 + i) + (lane & 1) * 16;
+      return i < mine - i0 && t < s_hi ? kv8_page(a.pool, x.b, t / kKv8Page) : -2;
     };
     int id = pages_at(0);
     Page<HD> buf[DEPTH][2];
@@ -119,7 +123,7 @@ __global__ void __launch_bounds__(256, (NT == 1 || !F32 ? 2 : 1)) k_kv8_attn(Kv8
     bool missing = false;   // a visible position has no page
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      const int c = c0 + 16 * nt + n16;
+      const int c = c0 + v0 + 16 * nt + n16;
       const bool on = c < nvec;
       const int row = x.s.beg + (on ? c / group : 0), h = g * group + (on ? c % group : 0);
       const long at = (long)row * a.ldq + (long)h * HD + qr * (HD / 4);
@@ -138,7 +142,6 @@ __global__ void __launch_bounds__(256, (NT == 1 || !F32 ? 2 : 1)) k_kv8_attn(Kv8
       l[nt] = 0.f;
     }
     lim_lo = wave_min_i(lim_lo);
-    lim_hi = wave_max_i(lim_hi);
 
     f32x4 acc[NT][DT];
 #pragma unroll
@@ -146,9 +149,6 @@ __global__ void __launch_bounds__(256, (NT == 1 || !F32 ? 2 : 1)) k_kv8_attn(Kv8
 #pragma unroll
       for (int d = 0; d < DT; ++d) acc[nt][d] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    const int p_hi = min(s_hi, lim_hi);
-    const int n_pairs = p_hi > p_lo ? (p_hi - p_lo + 31) / 32 : 0;
-    const int mine = n_pairs > wave ? (n_pairs - wave + 3) / 4 : 0;
     float eref = 0.f;     // largest value scale so far (0: none)
     for (int i0 = 0; i0 < mine; i0 += 32) {
       const int todo = min(32, mine - i0);
@@ -180,11 +180,11 @@ __global__ void __launch_bounds__(256, (NT == 1 || !F32 ? 2 : 1)) k_kv8_attn(Kv8
       const float rel = eref > 0.f ? sv / eref : 0.f;
 
       auto step = [&](Page<HD>(&pg)[2], int i) {
-        const int t0 = p_lo + (wave + 4 * (i0 + i)) * 32;
+        const int t0 = pair_at(i0 + i);
         const float ska = lane_f(sk, 2 * i), skb = lane_f(sk, 2 * i + 1);
         const float rva = lane_f(rel, 2 * i), rvb = lane_f(rel, 2 * i + 1);
         const bool oka = lane_i(ok, 2 * i) != 0, okb = lane_i(ok, 2 * i + 1) != 0;
-        const bool whole = t0 + 32 <= min(lim_lo, p_hi) && oka && okb;
+        const bool whole = t0 + 32 <= min(lim_lo, s_hi) && oka && okb;
         f32x4 sc[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) sc[nt][0] = sc[nt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -222,7 +222,7 @@ __global__ void __launch_bounds__(256, (NT == 1 || !F32 ? 2 : 1)) k_kv8_attn(Kv8
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
             if (!whole) {
-              const uint32_t v = sight_now(a, x, c0 + 16 * nt + n16, group, lim[nt], t0) & in_pair(p_hi - t0, oka, okb);
+              const uint32_t v = sight_now(a, x, c0 + v0 + 16 * nt + n16, group, lim[nt], t0) & in_pair(s_hi - t0, oka, okb);
               mask_scores(sc[nt][0], v, qr);
               mask_scores(sc[nt][1], v >> 16, qr);
             }
@@ -279,17 +279,17 @@ __global__ void __launch_bounds__(256, (NT == 1 || !F32 ? 2 : 1)) k_kv8_attn(Kv8
       l[nt] += xor_lane_c(l[nt], 16);
       l[nt] += xor_lane_c(l[nt], 32);
       if (qr == 0) {
-        sm_m[wave][16 * nt + n16] = m[nt];
-        sm_l[wave][16 * nt + n16] = l[nt];
+        sm_m[wave][v0 + 16 * nt + n16] = m[nt];
+        sm_l[wave][v0 + 16 * nt + n16] = l[nt];
       }
 #pragma unroll
       for (int d = 0; d < DT; ++d)
-        *reinterpret_cast<float4*>(&sm_o[wave][16 * nt + n16][16 * d + 4 * qr]) =
+        *reinterpret_cast<float4*>(&sm_o[wave][v0 + 16 * nt + n16][16 * d + 4 * qr]) =
             make_float4(acc[nt][d][0] * eref, acc[nt][d][1] * eref, acc[nt][d][2] * eref, acc[nt][d][3] * eref);
     }
     __syncthreads();
 #pragma unroll 1
-    for (int i = threadIdx.x; i < COLS * HD / 4; i += 256) {
+    for (int i = threadIdx.x; i < COLS * HD / 4; i += 256 * CT) {
       const int j = i / (HD / 4), e = i % (HD / 4) * 4, c = c0 + j;
       if (c >= nvec) break;   // (j ascends)
       float M = kNoMax;
@@ -390,41 +390,49 @@ __global__ void __launch_bounds__(256) k_kv8_join(Kv8AttnArgs a) {
   }
 }
 
-template <int HD, int NT>
+template <int HD, int NT, int CT>
 void launch_cols(const Kv8AttnArgs& a, dim3 grid, hipStream_t st) {
+  const dim3 block(256 * CT);
   if (a.x_bf16) {
-    if (a.stream) hipLaunchKernelGGL((k_kv8_attn<HD, NT, false, true>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((k_kv8_attn<HD, NT, false, false>), grid, dim3(256), 0, st, a);
+    if (a.stream) hipLaunchKernelGGL((k_kv8_attn<HD, NT, CT, false, true>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((k_kv8_attn<HD, NT, CT, false, false>), grid, block, 0, st, a);
   } else {
-    if (a.stream) hipLaunchKernelGGL((k_kv8_attn<HD, NT, true, true>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((k_kv8_attn<HD, NT, true, false>), grid, dim3(256), 0, st, a);
+    if (a.stream) hipLaunchKernelGGL((k_kv8_attn<HD, NT, CT, true, true>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((k_kv8_attn<HD, NT, CT, true, false>), grid, block, 0, st, a);
   }
 }
-
-// Sequences of at most 32 query vectors a kv head go to the kernel here, more to kv8_prompt.hip.
-bool use_prompt(int group, int max_rows) { return (long)group * max_rows > 32; }
-int cols_nt(int group, int max_rows) { return (long)group * max_rows <= 16 ? 1 : 2; }
+template <int HD>
+void launch_form(const Kv8AttnArgs& a, int form, dim3 grid, hipStream_t st) {
+  if (form == kKv8Narrow) launch_cols<HD, 1, 1>(a, grid, st);
+  else if (form == kKv8Shared) launch_cols<HD, 1, 2>(a, grid, st);
+  else launch_cols<HD, 2, 1>(a, grid, st);
+}
 
 }  // namespace
 
-int kv8_attention_cols(int x_bf16, int group, int max_rows) {
-  return use_prompt(group, max_rows) ? kv8_prompt_cols(x_bf16) : 16 * cols_nt(group, max_rows);
+// Up to 16 query vectors a kv head and sequence: one 16-column tile.  17 to 32: two tiles, either a
+// wavefront each over the same pages (8 wavefronts a block: less code and no registers spilled, but
+// every page converted twice and half as many pages in flight) or both in one wavefront.  Which, goes by
+// the (kv head, position) pairs of the pass.  8 rows of 4 heads, us, each / both, with 128-wide heads:
+// 8 sequences of 2000 positions and 8 kv heads 18 / 24, 8 of 3950 26 / 28, 10 of 3950 32 / 32, 12 of 3950
+// 39 / 34, 64 of 2300 124 / 74, 32 of 3950 and 2 kv heads 27 / 29, 64 so 47 / 39; 64-wide: 8 of 3950 and
+// 8 kv heads 15.6 / 15.7, 32 of 3950 34 / 32.  fp32, where both in one leave one wavefront a SIMD: 8 of
+// 3950 27 / 36, 16 of 3950 47 / 46, 64 of 2300 128 / 82.  More vectors: kv8_prompt.hip.
+int kv8_attention_form(int x_bf16, int group, int max_rows, long positions, int nkv) {
+  const long c = (long)group * max_rows;
+  if (c <= 16) return kKv8Narrow;
+  if (c > 32) return kKv8Prompt;
+  return positions * nkv <= (x_bf16 ? 1 << 18 : 1 << 19) ? kKv8Shared : kKv8Both;
 }
 
-void launch_kv8_attention(const Kv8AttnArgs& a, int max_rows, hipStream_t st) {
-  const int group = a.nq / a.pool.nkv, nt = cols_nt(group, max_rows);
+void launch_kv8_attention(const Kv8AttnArgs& a, hipStream_t st) {
   long y = (long)a.tiles * a.n_split;
   if (a.by_units) y = a.items;
   else if (a.split_len == 0 && a.n_split > 1) y = std::min<long>(y, (long)a.items + a.tiles);
   const dim3 grid(a.pool.nkv, (unsigned)std::min<long>(std::max<long>(y, 1), 65535));
-  if (use_prompt(group, max_rows)) return launch_kv8_prompt(a, grid, st);
-  if (a.hd == 128) {
-    if (nt == 1) launch_cols<128, 1>(a, grid, st);
-    else launch_cols<128, 2>(a, grid, st);
-  } else {
-    if (nt == 1) launch_cols<64, 1>(a, grid, st);
-    else launch_cols<64, 2>(a, grid, st);
-  }
+  if (a.form == kKv8Prompt) return launch_kv8_prompt(a, grid, st);
+  if (a.hd == 128) launch_form<128>(a, a.form, grid, st);
+  else launch_form<64>(a, a.form, grid, st);
 }
 
 void launch_kv8_join(const Kv8AttnArgs& a, hipStream_t st) {

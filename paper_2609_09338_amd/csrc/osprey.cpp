@@ -528,7 +528,8 @@ void run_kv8_attention(osprey_handle* h, const AttnArgs& a) {
   k.scale = 1.f;
   k.n_split = a.n_split;
   k.split_len = a.split_len;
-  const int cols = kv8_attention_cols(k.x_bf16, a.nq / a.nkv, a.rows_per_seq);
+  k.form = kv8_attention_form(k.x_bf16, a.nq / a.nkv, a.rows_per_seq, (long)a.B * a.n_split * a.split_len, a.nkv);
+  const int cols = kv8_form_cols(k.form, k.x_bf16);
   k.tiles = (int)((long)a.rows.max_rows * (a.nq / a.nkv) / cols) + a.B;
   k.stream = a.kv_stream;
   k.part = a.part;
@@ -538,7 +539,7 @@ void run_kv8_attention(osprey_handle* h, const AttnArgs& a) {
     k.o_lo = a.o_lo;
   }
   k.err = a.err;
-  launch_kv8_attention(k, a.rows_per_seq, h->stream);
+  launch_kv8_attention(k, h->stream);
 }
 
 // Attention over the cache and the merge of its context splits.  Timed (family 1),

@@ -310,6 +310,17 @@ def random_masks(rows, rng, empty=0.1):
     return out
 
 
+@pytest.mark.parametrize("max_context", [1, 1 << 20])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_attention_of_17_to_32_vectors_in_both_forms(dtype, hd, max_context):
+    cached, rows = [1500, 0, 31, 700], [8, 1, 5, 7]
+    cache = make_cache(4, 100, 2, hd, 7)
+    fill(cache, [c + r for c, r in zip(cached, rows)], gen_of(3))
+    check_attention(cache, cached, rows, dtype, gen_of(4), 8, max_context=max_context)
+    check_attention(cache, cached, rows, dtype, gen_of(5), 6, masks=random_masks(rows, random.Random(6)), max_context=max_context)
+
+
 @pytest.mark.parametrize("heads,dtype,cached,rows", [
     ((32, 8, 64), BF, [300, 1000, 0], [33, 65, 65]),
     ((16, 8, 128), F32, [17, 0], [16, 128]),
