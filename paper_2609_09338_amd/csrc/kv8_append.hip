@@ -517,22 +517,31 @@ __global__ void __launch_bounds__(256) k_kv8_append(Kv8AppendArgs a, int units, 
   }
 }
 
-// One wavefront per (sequence, kv head, keys or values): the positions base .. base + n - 1 take
-// the codes of base + path[i], page after page.  path ascends, so a position's source lies at or
-// behind it: reading a page's sources before writing it, in ascending order, moves in place.
+// One block per (sequence, kv head, keys or values): the positions base .. base + n - 1 take the
+// codes of base + path[i], a page a wavefront.  path ascends, so a position's source lies at or behind
+// it: no page's write reaches the sources of a later page, and once the block has read the sources
+// of its pages it may write them in place.
+// Bound by the round trips of a page (path, page table, scale and codes, older codes): 64 sequences'
+// paths over cold pages 13.5 us (the nodes of trees of 17 to 65), page after page 15.4; one short path 5 us.
 template <int HD>
-__global__ void __launch_bounds__(64) k_kv8_keep(Kv8KeepArgs a) {
+__global__ void __launch_bounds__(256) k_kv8_keep(Kv8KeepArgs a) {
   constexpr int NE = HD / 8, ND = HD / 32;
-  const int lane = threadIdx.x, b = blockIdx.x, g = blockIdx.y >> 1, kind = blockIdx.y & 1;
+  __shared__ int sm_bad;   // the first page that ends the move
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int b = blockIdx.x, g = blockIdx.y >> 1, kind = blockIdx.y & 1;
   const Lanes<HD> L(lane);
   const int base = a.base[b], n = min(a.n[b], a.ld);
   const int32_t* path = a.path + (long)b * a.ld;
   if (n <= 0 || base < 0) return;
   auto block = [&](int id) { return a.pool.codes + (long)id * a.pool.page_stride + ((long)kind * a.pool.nkv + g) * (kKv8Page * HD); };
   auto scale = [&](int id) { return a.pool.scales + (long)id * a.pool.scale_stride + 2 * g + kind; };
-  for (int pg = base / kKv8Page; pg * kKv8Page < base + n; ++pg) {
+  if (threadIdx.x == 0) sm_bad = 0x7fffffff;
+  __syncthreads();
+  for (int pg0 = base / kKv8Page; pg0 * kKv8Page < base + n; pg0 += 4) {
+    const int pg = pg0 + wave;
+    const bool on = pg * kKv8Page < base + n;
     const int lo = max(base, pg * kKv8Page), hi = min(base + n, (pg + 1) * kKv8Page), off = lo - pg * kKv8Page;
-    const int id = kv8_page(a.pool, b, pg);
+    const int id = on ? kv8_page(a.pool, b, pg) : -1;
     // source of position pg * 16 + t: its page, token there, and whether it is one
     auto source = [&](int t, int& tok) {
       const int i = pg * kKv8Page + t - base;
@@ -542,7 +551,8 @@ __global__ void __launch_bounds__(64) k_kv8_keep(Kv8KeepArgs a) {
       tok = (base + at) % kKv8Page;
       return kv8_page(a.pool, b, (base + at) / kKv8Page);
     };
-    bool bad = id < 0;
+    bool bad = on && id < 0;
+    const float old = id >= 0 && off > 0 ? *scale(id) : 0.f;
     double amax = 0.0;
     float x[2 * NE];                 // keys
     float y[4][2][ND];               // values
@@ -586,29 +596,32 @@ __global__ void __launch_bounds__(64) k_kv8_keep(Kv8KeepArgs a) {
       }
     }
     // (a page without a place, or a path that does not ascend: this sequence's move ends here)
-    if (__builtin_amdgcn_ballot_w64(bad)) {
-      if (lane == 0 && a.err) atomicOr(a.err, 1u << 3);
-      return;
-    }
+    if (__builtin_amdgcn_ballot_w64(bad) && lane == 0) atomicMin(&sm_bad, pg);
     amax = wave_max_d(amax);
-    const int was = off > 0 ? exp_of(*scale(id)) : kKv8MinExp;
-    const int e = max(scale_exp(amax), was);
-    const float f0 = kv8_pow2(-e / 2), f1 = kv8_pow2(-e - (-e / 2)), older = kv8_pow2(max(was - e, -126));
-    if (kind == 0) {
-      if (off > 0 && e > was) shift_keys<HD>(block(id), L, off, older);
+    __syncthreads();   // the sources are read
+    const int end = sm_bad;   // (or a page of the next round, which a faster wavefront has found)
+    if (pg == end && lane == 0 && a.err) atomicOr(a.err, 1u << 3);
+    if (on && pg < end) {
+      const int was = off > 0 ? exp_of(old) : kKv8MinExp;
+      const int e = max(scale_exp(amax), was);
+      const float f0 = kv8_pow2(-e / 2), f1 = kv8_pow2(-e - (-e / 2)), older = kv8_pow2(max(was - e, -126));
+      if (kind == 0) {
+        if (off > 0 && e > was) shift_keys<HD>(block(id), L, off, older);
 #pragma unroll
-      for (int i = 0; i < 2 * NE; ++i) x[i] = x[i] * f0 * f1;
-      if (L.t >= off && L.t < off + hi - lo) store_keys<HD>(block(id), L, x);
-    } else {
+        for (int i = 0; i < 2 * NE; ++i) x[i] = x[i] * f0 * f1;
+        if (L.t >= off && L.t < off + hi - lo) store_keys<HD>(block(id), L, x);
+      } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int o = 0; o < 2; ++o)
+          for (int o = 0; o < 2; ++o)
 #pragma unroll
-          for (int d = 0; d < ND; ++d) y[i][o][d] = y[i][o][d] * f0 * f1;
-      store_values<HD>(block(id), L, off, off + hi - lo, older, off > 0 && e > was, y);
+            for (int d = 0; d < ND; ++d) y[i][o][d] = y[i][o][d] * f0 * f1;
+        store_values<HD>(block(id), L, off, off + hi - lo, older, off > 0 && e > was, y);
+      }
+      if (lane == 0) *scale(id) = kv8_pow2(e);
     }
-    if (lane == 0) *scale(id) = kv8_pow2(e);
+    if (end < pg0 + 4) return;
   }
 }
 
@@ -645,8 +658,8 @@ void launch_kv8_append(const Kv8AppendArgs& a, hipStream_t st) {
 
 void launch_kv8_keep(const Kv8KeepArgs& a, hipStream_t st) {
   const dim3 grid(a.B, 2 * a.pool.nkv);
-  if (a.hd == 128) hipLaunchKernelGGL(k_kv8_keep<128>, grid, dim3(64), 0, st, a);
-  else hipLaunchKernelGGL(k_kv8_keep<64>, grid, dim3(64), 0, st, a);
+  if (a.hd == 128) hipLaunchKernelGGL(k_kv8_keep<128>, grid, dim3(256), 0, st, a);
+  else hipLaunchKernelGGL(k_kv8_keep<64>, grid, dim3(256), 0, st, a);
 }
 
 }  // namespace osp

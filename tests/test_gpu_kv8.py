@@ -416,6 +416,25 @@ def test_keep_moves_an_accepted_path(hd, nkv, base, paths):
     assert int(err) == 0
 
 
+def test_keep_of_paths_over_many_pages_ends_at_the_page_of_a_bad_step():
+    base, N = [5, 0, 16, 11], 200
+    cache = make_cache(4, 14, 2, 64, 5)
+    fill(cache, [b + N for b in base], gen_of(33), key_scale=3.0)
+    ref = ref_of(cache)
+    paths = [list(range(0, 200, 2)), list(range(40, 200)), list(range(8)) + list(range(90, 180)), [i + i // 3 for i in range(140)]]
+    paths[3][100] = paths[3][99]                        # position 111, the page of 96 to 111
+    rows = torch.full((4, 160), -1, dtype=torch.int32, device=DEV)
+    for b, p in enumerate(paths):
+        rows[b, :len(p)] = ints(p)
+    err = ints([0])
+    bd().kv8_keep(cache, ints(base), rows, ints([len(p) for p in paths]), errors=err)
+    for b, p in enumerate(paths):
+        kept = p if b < 3 else p[:96 - 11]
+        ref.keep(b, base[b], kept)
+        same_cache(cache, ref, b, base[b] + len(kept))
+    assert int(err) == 1 << 3
+
+
 def test_keep_refuses_a_path_that_does_not_ascend():
     cache = make_cache(2, 4, 1, 64, 5)
     fill(cache, [64, 64], gen_of(1))
