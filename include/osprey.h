@@ -431,8 +431,9 @@ int osprey_graph_destroy(osprey_graph* g);
  *
  * Device conditions (err, nullable, a device word that the calls only set bits of): bit 2 a
  * row sees positions without a page (skipped), bit 3 a write to a position without a page
- * (skipped) or a kept path that does not ascend, bit 6 a key or value that is not finite
- * (stored as zero), bit 7 a rotation position outside the table (clamped). */
+ * (skipped) or a kept path that does not ascend (either ends that sequence's move at its
+ * page), bit 6 a key or value that is not finite (stored as zero), bit 7 a rotation position
+ * outside the table (clamped). */
 typedef struct {
   const int32_t* page_table;  /* [batch][max_pages] */
   int32_t batch;              /* sequences: 1 .. 4096 */

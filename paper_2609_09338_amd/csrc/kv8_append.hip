@@ -521,8 +521,8 @@ __global__ void __launch_bounds__(256) k_kv8_append(Kv8AppendArgs a, int units, 
 // codes of base + path[i], a page a wavefront.  path ascends, so a position's source lies at or behind
 // it: no page's write reaches the sources of a later page, and once the block has read the sources
 // of its pages it may write them in place.
-// Bound by the round trips of a page (path, page table, scale and codes, older codes): 64 sequences'
-// paths over cold pages 13.5 us (the nodes of trees of 17 to 65), page after page 15.4; one short path 5 us.
+// Bound by the round trips of a page (path, page table, scale and codes, older codes): paths of up to
+// 9 positions of 64 sequences, cold pages, 13.5 us (page after page 15.4); one path 5 us.
 template <int HD>
 __global__ void __launch_bounds__(256) k_kv8_keep(Kv8KeepArgs a) {
   constexpr int NE = HD / 8, ND = HD / 32;
@@ -532,7 +532,11 @@ __global__ void __launch_bounds__(256) k_kv8_keep(Kv8KeepArgs a) {
   const Lanes<HD> L(lane);
   const int base = a.base[b], n = min(a.n[b], a.ld);
   const int32_t* path = a.path + (long)b * a.ld;
-  if (n <= 0 || base < 0) return;
+  if (n <= 0) return;
+  if (base < 0 || base > kKv8MaxPos - n) {
+    if (threadIdx.x == 0 && a.err) atomicOr(a.err, 1u << 3);
+    return;
+  }
   auto block = [&](int id) { return a.pool.codes + (long)id * a.pool.page_stride + ((long)kind * a.pool.nkv + g) * (kKv8Page * HD); };
   auto scale = [&](int id) { return a.pool.scales + (long)id * a.pool.scale_stride + 2 * g + kind; };
   if (threadIdx.x == 0) sm_bad = 0x7fffffff;

@@ -447,6 +447,17 @@ def test_keep_refuses_a_path_that_does_not_ascend():
     assert int(err) == 1 << 3
 
 
+def test_keep_refuses_places_that_are_none():
+    cache = make_cache(3, 4, 1, 64, 5)
+    fill(cache, [64, 64, 64], gen_of(1))
+    ref = ref_of(cache)
+    err = ints([0])
+    bd().kv8_keep(cache, ints([-1, 2**31 - 1, 4]), ints([[0, 1]] * 3), ints([2, 2, 0]), errors=err)
+    for b in range(3):
+        same_cache(cache, ref, b, 64)
+    assert int(err) == 1 << 3
+
+
 def test_a_tree_verified_kept_and_continued():
     """A layer's calls as a target makes them: prompt, tree rows, their mask, the accepted path, the
     next token; every attention against the reference cache that went through the same steps."""
