@@ -449,7 +449,8 @@ typedef struct {
 
 /* Arguments of osprey_kv8_append.  Sequence b has rows cu_rows[b] .. cu_rows[b + 1] - 1 of
  * `rows` (cu_rows NULL: one row each, rows == batch), which take the positions cached[b],
- * cached[b] + 1, ...  Rows behind cu_rows[batch] are neither read nor written.
+ * cached[b] + 1, ...  Rows before cu_rows[0] and behind cu_rows[batch] are neither read nor
+ * written.
  * Queries and keys are normalised per head (x gain / sqrt(mean x^2 + eps), where the gain is
  * given) and rotated by halves with the cosines and sines of the row's position (rope_pos, or
  * the cache position where that is NULL; rope_cos NULL: no rotation); queries go to q_out,

@@ -73,6 +73,8 @@ OSP_DEV float to_float_odd(double x) {
   return __int_as_float(i);
 }
 
+constexpr double kFloatMax = 3.4028234663852886e38;   // (below 448 2^kKv8MaxExp)
+
 // Smallest E in [kKv8MinExp, kKv8MaxExp] with amax <= 448 2^E.
 OSP_DEV int scale_exp(double amax) {
   int e = kKv8MinExp;
@@ -239,7 +241,7 @@ OSP_DEV void append_keys(const Kv8AppendArgs& a, int b, const Kv8Seq& s, int r0,
   double amax = 0.0;
 #pragma unroll
   for (int i = 0; i < 2 * NE; ++i) {
-    if (!(fabs(x[i]) < 1.0e300)) {   // not finite (a finite input cannot come near this)
+    if (!(fabs(x[i]) <= kFloatMax)) {   // not finite, or not so once its gain has been applied
       x[i] = 0.0;
       bad = true;
     }
@@ -335,10 +337,12 @@ OSP_DEV void do_queries(const Kv8AppendArgs& a, int row0, int rows, int h0, int 
   }
 #pragma unroll
   for (int r = 0; r < RQ; ++r) pos[r] = rope_row(a, min(row0 + r, rows - 1));
+  const int first = a.r.cu ? a.r.cu[0] : 0;
 #pragma unroll
   for (int r = 0; r < RQ; ++r) {
     const int row = row0 + r;
     if (row >= rows) return;
+    if (row < first) continue;
     float* x = xs[r];
     if (a.q_norm) {
       float ss = 0.f;
@@ -441,7 +445,7 @@ __global__ void __launch_bounds__(256) k_kv8_append_one(Kv8AppendArgs a, int uni
   float vmax = 0.f;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    if (!(fabs(kv[i]) < 1.0e300)) { kv[i] = 0.0; bad = true; }
+    if (!(fabs(kv[i]) <= kFloatMax)) { kv[i] = 0.0; bad = true; }
     if (!(fabsf(f[2 + i]) < INFINITY)) { f[2 + i] = 0.f; bad = true; }
     kmax = fmax(kmax, fabs(kv[i]));
     vmax = fmaxf(vmax, fabsf(f[2 + i]));
@@ -523,6 +527,8 @@ __global__ void __launch_bounds__(256) k_kv8_append(Kv8AppendArgs a, int units, 
 // of its pages it may write them in place.
 // Bound by the round trips of a page (path, page table, scale and codes, older codes): paths of up to
 // 9 positions of 64 sequences, cold pages, 13.5 us (page after page 15.4); one path 5 us.
+// Values are carried at 2^-16 of theirs: 256 2^120, to which the largest floats round, is none.
+constexpr float kKeepDown = 1.f / 65536.f;
 template <int HD>
 __global__ void __launch_bounds__(256) k_kv8_keep(Kv8KeepArgs a) {
   constexpr int NE = HD / 8, ND = HD / 32;
@@ -567,7 +573,7 @@ __global__ void __launch_bounds__(256) k_kv8_keep(Kv8KeepArgs a) {
 #pragma unroll
       for (int i = 0; i < 2 * NE; ++i) x[i] = 0.f;
       if (src >= 0) {
-        const float f = *scale(src);
+        const float f = *scale(src) * kKeepDown;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const uint32_t* p = reinterpret_cast<const uint32_t*>(block(src) + tok * HD + h * (HD / 2) + L.j * NE);
@@ -586,7 +592,7 @@ __global__ void __launch_bounds__(256) k_kv8_keep(Kv8KeepArgs a) {
         int tok = 0;
         const int src = source(4 * L.q + i, tok);
         bad |= src == -1;
-        const float f = src >= 0 ? *scale(src) : 0.f;
+        const float f = src >= 0 ? *scale(src) * kKeepDown : 0.f;
         const uint8_t* p = block(max(src, 0)) + (tok / 4) * 4 * HD + tok % 4;
 #pragma unroll
         for (int o = 0; o < 2; ++o)
@@ -607,8 +613,8 @@ __global__ void __launch_bounds__(256) k_kv8_keep(Kv8KeepArgs a) {
     if (pg == end && lane == 0 && a.err) atomicOr(a.err, 1u << 3);
     if (on && pg < end) {
       const int was = off > 0 ? exp_of(old) : kKv8MinExp;
-      const int e = max(scale_exp(amax), was);
-      const float f0 = kv8_pow2(-e / 2), f1 = kv8_pow2(-e - (-e / 2)), older = kv8_pow2(max(was - e, -126));
+      const int e = max(scale_exp(amax / kKeepDown), was), up = 16 - e;
+      const float f0 = kv8_pow2(up / 2), f1 = kv8_pow2(up - up / 2), older = kv8_pow2(max(was - e, -126));
       if (kind == 0) {
         if (off > 0 && e > was) shift_keys<HD>(block(id), L, off, older);
 #pragma unroll

@@ -341,7 +341,7 @@ __global__ void __launch_bounds__(256) k_kv8_join(Kv8AttnArgs a) {
   const int i = blockIdx.x * G + wave / W, part = wave % W;
   const int row = i / a.nq, h = i % a.nq;
   const int total = a.r.count ? min(*a.r.count, a.r.rows) : a.r.rows;
-  const bool on = row < total && !(a.r.cu && row >= a.r.cu[a.r.B]);
+  const bool on = row < total && !(a.r.cu && (row < a.r.cu[0] || row >= a.r.cu[a.r.B]));
   const int ns = on ? min(a.row_ns[i], a.n_split) : 0;
   float o[E] = {}, L = 0.f;
   if (ns > 1) {   // (else written by the attention itself)

@@ -482,7 +482,7 @@ Kv8Pool kv8_pool(const osprey_handle* h, int layer, int slot0, const int32_t* bs
 }
 
 // Whether an 8-bit handle's pass attends by tiles of many query vectors, which take bf16 queries
-// (their rounding, 2^-9, is far below the codes', 2^-4; the few rows of a draft step keep fp32).
+// (their rounding, 2^-8, is far below the codes', 2^-4; the few rows of a draft step keep fp32).
 bool kv8_many(const AttnArgs& a) { return !a.tree_node && (a.nq / a.nkv) * (long)a.rows_per_seq > 32; }
 
 // launch_rows_qkv of an 8-bit handle (draft-tree rows keep their own bf16 cache).

@@ -134,6 +134,38 @@ def test_append_writes_the_codes_of_the_definition(heads, dtype, cached, rows, g
         assert bool((out[n:] == 7.0).all()), "rows behind the last sequence were written"
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("first", [3, 40])
+def test_rows_before_the_first_sequence_and_behind_the_last_are_left_as_they_are(dtype, first):
+    """The sequences of a pass may be a part of a packed batch."""
+    hd, nq, nkv, rows = 64, 4, 2, [5, 20]
+    lo, hi, n = first, first + 25, first + 25 + 9
+    cache, other = make_cache(2, 4, nkv, hd, 5), make_cache(2, 4, nkv, hd, 5)
+    for c in (cache, other):
+        fill(c, [60, 60], gen_of(9))
+    gen = gen_of(8)
+    k, v, q = (torch.randn((n, h, hd), generator=gen, device=DEV).to(dtype) for h in (nkv, nkv, nq))
+    q_out = torch.full_like(q, 7.0)
+    cos, sin = (t.to(DEV) for t in tables(64, hd))
+    cu = ints([lo, lo + rows[0], hi])
+    kw = dict(rope_cos=cos, rope_sin=sin)
+    bd().kv8_append(cache, k, v, ints([0, 30]), q=q, q_out=q_out, cu_rows=cu, **kw)
+    part = torch.full_like(q[lo:hi], 7.0)
+    at = ints([0, rows[0], 25])
+    bd().kv8_append(other, k[lo:hi], v[lo:hi], ints([0, 30]), q=q[lo:hi], q_out=part, cu_rows=at, **kw)
+    assert torch.equal(cache.codes, other.codes) and torch.equal(q_out[lo:hi], part)
+    assert bool((q_out[:lo] == 7.0).all()) and bool((q_out[hi:] == 7.0).all())
+    for rows_of in (1, 64):                  # either kernel, joined and not
+        for ctx in (1, 1000):
+            out, want = torch.full_like(q, 7.0), torch.empty_like(part)
+            for o, x, c, m in ((out, q_out, cu, n), (want, part, at, 25)):
+                ws = torch.full((bd().kv8_attention_workspace(cache, m, nq, rows_of, ctx),), 1, dtype=torch.uint8, device=DEV)
+                bd().kv8_attention(cache, x, o, ints([0, 30]), ws, max_rows=rows_of, max_context=ctx, cu_rows=c)
+            # (the plans may differ with the row count: last bits)
+            assert bool((out[:lo] == 7.0).all()) and bool((out[hi:] == 7.0).all())
+            assert float((out[lo:hi].float() - want.float()).abs().max()) <= 2.0 ** -6 * float(want.float().abs().max())
+
+
 def test_append_token_by_token_grows_scales_as_one_call_each():
     """Forty calls of one row each, magnitudes rising and falling by powers of two."""
     nkv, hd = 2, 64
@@ -445,6 +477,42 @@ def test_keep_refuses_a_path_that_does_not_ascend():
     same_cache(cache, ref, 0, 64)
     same_cache(cache, ref, 1, 6)
     assert int(err) == 1 << 3
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_the_largest_floats_are_kept_and_moved(hd):
+    cache = make_cache(2, 3, 2, hd, 5)
+    top = torch.finfo(BF).max                # rounds to 256 2^120, which is no float
+    k = torch.randn((80, 2, hd), generator=gen_of(2), device=DEV).to(BF)
+    v = torch.randn((80, 2, hd), generator=gen_of(3), device=DEV).to(BF)
+    k[5, 0, 3], k[21, 1, 7], v[9, 1, 0], v[50, 0, hd - 1] = top, -top, top, top
+    ref = ref_of(cache)
+    err = ints([0])
+    bd().kv8_append(cache, k, v, ints([0, 0]), cu_rows=ints([0, 40, 80]), errors=err)
+    for b in range(2):
+        ref.write(b, 0, k[40 * b:40 * b + 40].cpu().double(), v[40 * b:40 * b + 40].cpu().double())
+        same_cache(cache, ref, b, 40)
+    bd().kv8_keep(cache, ints([3, 8]), ints([[0, 2, 6, 18, 20], [1, 2, 7, 8, 9]]), ints([5, 5]), errors=err)
+    ref.keep(0, 3, [0, 2, 6, 18, 20])
+    ref.keep(1, 8, [1, 2, 7, 8, 9])
+    same_cache(cache, ref, 0, 8)
+    same_cache(cache, ref, 1, 13)
+    assert int(err) == 0
+
+
+@pytest.mark.parametrize("rows", [1, 20])
+def test_keys_that_their_gain_takes_past_the_floats_are_stored_as_zeros(rows):
+    hd = 64
+    cache = make_cache(1, 3, 1, hd, 5)
+    k = torch.zeros((rows, 1, hd), device=DEV)
+    k[:, 0, 0] = 1.0                         # normalised: 8 in dim 0
+    v = torch.ones((rows, 1, hd), device=DEV)
+    gain = torch.full((hd,), 1.0e38, device=DEV)
+    err = ints([0])
+    bd().kv8_append(cache, k, v, ints([0]), cu_rows=ints([0, rows]) if rows > 1 else None, k_norm=gain, errors=err)
+    ref = ref_of(cache)
+    keys, values = ref.context(0, rows)
+    assert int(err) == 1 << 6 and bool((keys == 0).all()) and bool((values == 1).all())
 
 
 def test_keep_refuses_places_that_are_none():
