@@ -274,18 +274,19 @@ __global__ void __launch_bounds__(256 * CT, NT == 1 || !F32 ? 2 : 1) k_kv8_attn(
 
     // ---- merge the wavefronts --------------------------------------------------------
     const bool direct = x.ns == 1 && a.out != nullptr;   // one split: no join
+    const float back = eref * kDownBy;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       l[nt] += xor_lane_c(l[nt], 16);
       l[nt] += xor_lane_c(l[nt], 32);
       if (qr == 0) {
         sm_m[wave][v0 + 16 * nt + n16] = m[nt];
-        sm_l[wave][v0 + 16 * nt + n16] = l[nt];
+        sm_l[wave][v0 + 16 * nt + n16] = l[nt] * kDownBy;
       }
 #pragma unroll
       for (int d = 0; d < DT; ++d)
         *reinterpret_cast<float4*>(&sm_o[wave][v0 + 16 * nt + n16][16 * d + 4 * qr]) =
-            make_float4(acc[nt][d][0] * eref, acc[nt][d][1] * eref, acc[nt][d][2] * eref, acc[nt][d][3] * eref);
+            make_float4(acc[nt][d][0] * back, acc[nt][d][1] * back, acc[nt][d][2] * back, acc[nt][d][3] * back);
     }
     __syncthreads();
 #pragma unroll 1
@@ -322,7 +323,7 @@ __global__ void __launch_bounds__(256 * CT, NT == 1 || !F32 ? 2 : 1) k_kv8_attn(
         *reinterpret_cast<float2*>(pp + 4 + e) = make_float2(o[2], o[3]);
         if (e == 0) {
           // (P was lifted by 2^kLift)
-          pp[0] = a.natural ? (M > kNoMax ? (M - kLift) * kLn2 : -INFINITY) : M;
+          pp[0] = a.natural ? (M > kNoMax ? (M - kLift + kDown) * kLn2 : -INFINITY) : M;
           pp[1] = L;
         }
       }

@@ -17,6 +17,9 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kNoMax = -1.0e30f;   // below any score: a row that has seen nothing
 constexpr float kLift = 6.f;         // P's largest value is 2^kLift, 2^(kLift + kSlack) before the maximum moves
 constexpr float kSlack = 8.f;
+// Sums and outputs leave a wavefront at 2^-kDown: P's lift and a long context's sum of it take them past
+// fp32 with values from 2^96 on, and nothing that counts falls below (a row's sum is 2^5 at least).
+constexpr float kDown = 24.f, kDownBy = 1.f / (1 << 24);
 
 OSP_DEV uint32_t h2(f16x2 v) { return __builtin_bit_cast(uint32_t, v); }
 // Two of a dword's codes as f16, times a power of two.

@@ -328,14 +328,15 @@ __global__ void __launch_bounds__(64 * NW, HD == 64 ? 3 : 2) k_kv8_prompt(Kv8Att
                                                              f32x2_to_bf16x2(acc[nt][d][2] * inv, acc[nt][d][3] * inv));
       } else {
         float* pp = a.part + (((long)row * a.nq + h) * a.n_split + x.split) * (HD + 2);
+        const float back = eref * kDownBy;
         if (qr == 0) {
-          pp[0] = a.natural ? (m[nt] > kNoMax ? (m[nt] - kLift) * kLn2 : -INFINITY) : m[nt];
-          pp[1] = l[nt];
+          pp[0] = a.natural ? (m[nt] > kNoMax ? (m[nt] - kLift + kDown) * kLn2 : -INFINITY) : m[nt];
+          pp[1] = l[nt] * kDownBy;
         }
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
-          *reinterpret_cast<float2*>(pp + 2 + 16 * d + 4 * qr) = make_float2(acc[nt][d][0] * eref, acc[nt][d][1] * eref);
-          *reinterpret_cast<float2*>(pp + 4 + 16 * d + 4 * qr) = make_float2(acc[nt][d][2] * eref, acc[nt][d][3] * eref);
+          *reinterpret_cast<float2*>(pp + 2 + 16 * d + 4 * qr) = make_float2(acc[nt][d][0] * back, acc[nt][d][1] * back);
+          *reinterpret_cast<float2*>(pp + 4 + 16 * d + 4 * qr) = make_float2(acc[nt][d][2] * back, acc[nt][d][3] * back);
         }
       }
     }

@@ -389,6 +389,17 @@ def test_attention_of_sharp_scores_and_of_blocks_of_very_different_scales():
         check_attention(cache, [n - 3], [3], dtype, gen, 4, scale=1e-3)
 
 
+@pytest.mark.parametrize("value_scale", [1.0e34, 1.0e-27])
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("rows", [1, 5, 40])
+def test_attention_of_values_near_the_ends_of_fp32(rows, dtype, value_scale):
+    cached = [2000, 30]
+    cache = make_cache(2, 130, 2, 64, 7)
+    fill(cache, [c + rows for c in cached], gen_of(3), value_scale=value_scale)
+    for max_context in (1, 4000):            # one split, several
+        check_attention(cache, cached, [rows, rows], dtype, gen_of(4), 8, q_scale=0.05, max_context=max_context)
+
+
 def test_attention_with_a_first_position_that_takes_most_of_the_weight():
     """The rest weighs 2^-13 a token and more than it in sum: probabilities far below the maximum count."""
     nkv, hd, n = 1, 64, 40000
