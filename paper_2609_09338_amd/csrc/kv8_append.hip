@@ -12,8 +12,12 @@
 // data, and the same codes whatever else is in the batch.
 // A code is a rounding to 4 bits: a key that is off by 2^-24 next to a border changes by a
 // sixteenth of itself.  Keys are therefore normalised and rotated in double (half of the fp32
-// rate here, and keys are the smaller part of a row), and rounded once: codes are those of the
-// definition, not of a summation order.  Values and queries need no more than fp32.
+// rate here), and rounded once: codes are those of the definition, not of a summation order.  fp32
+// queries are formed so too (6.3e-8 of their size off in fp32, a rounding's 2.5e-8 so; 6000 rows of
+// 32 heads 60 and 62 us); bf16 queries, whose rounding is 2^-8, in fp32 (8000 rows of 32 heads of 64
+// 31 us, in double 38), and values need no more.
+#include <type_traits>
+
 #include "kv8.h"
 
 namespace osp {
@@ -319,6 +323,9 @@ OSP_DEV int rope_row(const Kv8AppendArgs& a, int row) {
   return a.r.cached[lo] + row - a.r.cu[lo];
 }
 
+template <int C> OSP_DEV float dpp(float v) { return dpp_f<C>(v); }
+template <int C> OSP_DEV double dpp(double v) { return dpp_d<C>(v); }
+
 // Queries of RQ rows from row0 on: HD / (2 V) lanes a head, V values of either half a lane; every
 // row's values are requested before the first is used.
 template <typename T, int HD, int RQ>
@@ -343,33 +350,41 @@ OSP_DEV void do_queries(const Kv8AppendArgs& a, int row0, int rows, int h0, int 
     const int row = row0 + r;
     if (row >= rows) return;
     if (row < first) continue;
-    float* x = xs[r];
+    typedef typename std::conditional<sizeof(T) == 4, double, float>::type acc_t;
+    acc_t x[2 * V];
+#pragma unroll
+    for (int i = 0; i < 2 * V; ++i) x[i] = xs[r][i];
     if (a.q_norm) {
-      float ss = 0.f;
+      acc_t ss = 0;
 #pragma unroll
       for (int i = 0; i < 2 * V; ++i) ss += x[i] * x[i];
-      ss += dpp_f<kDppXor1>(ss);
-      ss += dpp_f<kDppXor2>(ss);
-      if constexpr (LPH >= 8) ss += dpp_f<kDppHalfMirror>(ss);
-      if constexpr (LPH >= 16) ss += dpp_f<kDppMirror>(ss);
-      const float inv = 1.0f / sqrtf(ss / HD + a.eps);
+      ss += dpp<kDppXor1>(ss);
+      ss += dpp<kDppXor2>(ss);
+      if constexpr (LPH >= 8) ss += dpp<kDppHalfMirror>(ss);
+      if constexpr (LPH >= 16) ss += dpp<kDppMirror>(ss);
+      acc_t inv;
+      if constexpr (sizeof(T) == 4) inv = 1.0 / sqrt(ss / HD + (double)a.eps);
+      else inv = 1.0f / sqrtf(ss / HD + a.eps);
 #pragma unroll
-      for (int i = 0; i < 2 * V; ++i) x[i] *= inv * gain(a.q_norm, a.g_bf16, (i / V) * (HD / 2) + j * V + i % V);
+      for (int i = 0; i < 2 * V; ++i) x[i] *= inv * (acc_t)gain(a.q_norm, a.g_bf16, (i / V) * (HD / 2) + j * V + i % V);
     }
     if (a.rope_cos) {
       const long c = (long)min(max(pos[r], 0), a.max_pos - 1) * (HD / 2) + j * V;
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        const float co = a.rope_cos[c + i], si = a.rope_sin[c + i], u = x[i], w = x[V + i];
+        const acc_t co = a.rope_cos[c + i], si = a.rope_sin[c + i], u = x[i], w = x[V + i];
         x[i] = u * co - w * si;
         x[V + i] = w * co + u * si;
       }
     }
+    float z[2 * V];
+#pragma unroll
+    for (int i = 0; i < 2 * V; ++i) z[i] = (float)x[i];
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       const long at = (long)row * a.ldo + (long)h * HD + k * (HD / 2) + j * V;
       T* o = reinterpret_cast<T*>(a.q_out) + at;
-      float* y = x + k * V;
+      const float* y = z + k * V;
       if constexpr (sizeof(T) == 2) {
         *reinterpret_cast<uint4*>(o) = make_uint4(f32x2_to_bf16x2(y[0] * a.q_scale, y[1] * a.q_scale), f32x2_to_bf16x2(y[2] * a.q_scale, y[3] * a.q_scale),
                                                   f32x2_to_bf16x2(y[4] * a.q_scale, y[5] * a.q_scale), f32x2_to_bf16x2(y[6] * a.q_scale, y[7] * a.q_scale));
