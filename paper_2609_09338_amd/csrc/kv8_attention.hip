@@ -17,7 +17,7 @@
 //     products) beside f16 codes.
 //   * A key block's scale and the softmax scale are one factor of the exponent's fma.  A value
 //     block's scale, relative to the largest of the wavefront's pages so far, is an operand of its
-//     codes' conversion.  P is held in f16 with 2^6 .. 2^14 as its largest value: 11 bits down to
+//     codes' conversion (scales that lie too far apart for f16: ValueUnit).  P is held in f16 with 2^6 .. 2^14 as its largest value: 11 bits down to
 //     2^-20 of it and an absolute 2^-31 below, where bf16's 8 bits would add an error of the output's
 //     own rounding.  fp32 rows take P as hi + lo as well.  Maxima, sums and outputs are fp32.
 //   * The running maximum only moves when a score passes it by 2^8 (one ballot a pair, no
@@ -149,108 +149,102 @@ __global__ void __launch_bounds__(256 * CT, NT == 1 || !F32 ? 2 : 1) k_kv8_attn(
 #pragma unroll
       for (int d = 0; d < DT; ++d) acc[nt][d] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    float eref = 0.f;     // largest value scale so far (0: none)
-    for (int i0 = 0; i0 < mine; i0 += 32) {
-      const int todo = min(32, mine - i0);
-      if (i0 > 0) {
-        id = pages_at(i0);
-#pragma unroll
-        for (int i = 0; i + 1 < DEPTH; ++i) request(buf[i], i);
-      }
-      float sk = 0.f, sv = 0.f;
+    ValueUnit unit;
+    float sk = 0.f, rel = 0.f;   // scales of the chunk's pages (keys; values: enter_scales)
+    int ok = 0;
+    auto enter = [&]() {
+      float sv = 0.f;
+      sk = 0.f;
       if (id >= 0) {
         const float* s = a.pool.scales + (long)id * a.pool.scale_stride + 2 * g;
         sk = s[0];
         sv = s[1];
       }
       missing |= id == -1;
-      const int ok = id >= 0;
-      // values are converted relative to the largest scale so far
-      const float top = fmaxf(eref, wave_max(fabsf(sv)));
-      if (top > eref) {
-        if (eref > 0.f) {
-          const float f = eref / top;
+      ok = id >= 0;
+      const float f = enter_scales(unit, sv, rel);
+      if (f != 1.f) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int d = 0; d < DT; ++d) acc[nt][d] *= f;
+      }
+    };
+    auto step = [&](Page<HD>(&pg)[2], int i0, int i, auto apart) {
+      const int t0 = pair_at(i0 + i);
+      const float ska = lane_f(sk, 2 * i), skb = lane_f(sk, 2 * i + 1);
+      const float rva = lane_f(rel, 2 * i), rvb = lane_f(rel, 2 * i + 1);
+      const bool oka = lane_i(ok, 2 * i) != 0, okb = lane_i(ok, 2 * i + 1) != 0;
+      const bool whole = t0 + 32 <= min(lim_lo, s_hi) && oka && okb;
+      f32x4 sc[NT][2];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) sc[nt][0] = sc[nt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int c = 0; c < KC; ++c) {
+          qk_t kf;
+          if constexpr (F32) kf = frag8(pg[k].kd(2 * c), pg[k].kd(2 * c + 1));
+          else kf = frag8_bf16(pg[k].kd(2 * c), pg[k].kd(2 * c + 1));
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int d = 0; d < DT; ++d) acc[nt][d] *= f;
+            for (int p = 0; p < NP; ++p) sc[nt][k] = mfma(kf, qf[nt][p][c], sc[nt][k]);
         }
-        eref = top;
-      }
-      const float rel = eref > 0.f ? sv / eref : 0.f;
-
-      auto step = [&](Page<HD>(&pg)[2], int i) {
-        const int t0 = pair_at(i0 + i);
-        const float ska = lane_f(sk, 2 * i), skb = lane_f(sk, 2 * i + 1);
-        const float rva = lane_f(rel, 2 * i), rvb = lane_f(rel, 2 * i + 1);
-        const bool oka = lane_i(ok, 2 * i) != 0, okb = lane_i(ok, 2 * i + 1) != 0;
-        const bool whole = t0 + 32 <= min(lim_lo, s_hi) && oka && okb;
-        f32x4 sc[NT][2];
+      float z[NT][8], top = -INFINITY;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) sc[nt][0] = sc[nt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int nt = 0; nt < NT; ++nt)
+        exponents(sc[nt], score_factor(ska, colc[nt]), score_factor(skb, colc[nt]), kLift - m[nt], z[nt], top);
+      // One branch for all that is rare: pairs that some vector sees in part, maxima that move.
+      if (!whole || __builtin_amdgcn_ballot_w64(top > kLift + kSlack)) {
+        if (!whole) {
+          // value codes past the context may be anything: 0 * NaN
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
+          for (int k = 0; k < 2; ++k) {
+            const int left = (k ? okb : oka) ? x.s.ctx - (t0 + 16 * k + 4 * qr) : 0;
+            const uint32_t keep = left >= 4 ? 0xffffffffu : left <= 0 ? 0u : (1u << 8 * left) - 1u;
 #pragma unroll
-          for (int c = 0; c < KC; ++c) {
-            qk_t kf;
-            if constexpr (F32) kf = frag8(pg[k].kd(2 * c), pg[k].kd(2 * c + 1));
-            else kf = frag8_bf16(pg[k].kd(2 * c), pg[k].kd(2 * c + 1));
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-              for (int p = 0; p < NP; ++p) sc[nt][k] = mfma(kf, qf[nt][p][c], sc[nt][k]);
-          }
-        float z[NT][8], top = -INFINITY;
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-          exponents(sc[nt], score_factor(ska, colc[nt]), score_factor(skb, colc[nt]), kLift - m[nt], z[nt], top);
-        // One branch for all that is rare: pairs that some vector sees in part, maxima that move.
-        if (!whole || __builtin_amdgcn_ballot_w64(top > kLift + kSlack)) {
-          if (!whole) {
-            // value codes past the context may be anything: 0 * NaN
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              const int left = (k ? okb : oka) ? x.s.ctx - (t0 + 16 * k + 4 * qr) : 0;
-              const uint32_t keep = left >= 4 ? 0xffffffffu : left <= 0 ? 0u : (1u << 8 * left) - 1u;
-#pragma unroll
-              for (int d = 0; d < HD / 64; ++d) {
-                uint4& v = pg[k].v[d];
-                v = make_uint4(v.x & keep, v.y & keep, v.z & keep, v.w & keep);
-              }
+            for (int d = 0; d < HD / 64; ++d) {
+              uint4& v = pg[k].v[d];
+              v = make_uint4(v.x & keep, v.y & keep, v.z & keep, v.w & keep);
             }
           }
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            if (!whole) {
-              const uint32_t v = sight_now(a, x, c0 + v0 + 16 * nt + n16, group, lim[nt], t0) & in_pair(s_hi - t0, oka, okb);
-              mask_scores(sc[nt][0], v, qr);
-              mask_scores(sc[nt][1], v >> 16, qr);
-            }
-            const float fa = score_factor(ska, colc[nt]), fb = score_factor(skb, colc[nt]);
-            float cm = fmaxf(max4(sc[nt][0]) * fa, max4(sc[nt][1]) * fb);
-            cm = fmaxf(cm, xor_lane_c(cm, 16));
-            cm = fmaxf(cm, xor_lane_c(cm, 32));
-            const float mn = cm > m[nt] + kSlack ? ceilf(cm) : m[nt];
-            const float w = exp2f(m[nt] - mn);
-            m[nt] = mn;
-            l[nt] *= w;
-#pragma unroll
-            for (int d = 0; d < DT; ++d) acc[nt][d] *= w;
-            exponents(sc[nt], fa, fb, kLift - m[nt], z[nt], top);
-          }
         }
-        f16x8 pf[NT][NP];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-          if constexpr (F32) {
-            probability_parts(z[nt], l[nt], pf[nt][0], pf[nt][NP - 1]);
-          } else {
-            uint32_t u[4];
-            probabilities(z[nt], l[nt], u);
-            probabilities(z[nt] + 4, l[nt], u + 2);
-            pf[nt][0] = frag(u[0], u[1], u[2], u[3]);
+          if (!whole) {
+            const uint32_t v = sight_now(a, x, c0 + v0 + 16 * nt + n16, group, lim[nt], t0) & in_pair(s_hi - t0, oka, okb);
+            mask_scores(sc[nt][0], v, qr);
+            mask_scores(sc[nt][1], v >> 16, qr);
           }
+          const float fa = score_factor(ska, colc[nt]), fb = score_factor(skb, colc[nt]);
+          float cm = fmaxf(max4(sc[nt][0]) * fa, max4(sc[nt][1]) * fb);
+          cm = fmaxf(cm, xor_lane_c(cm, 16));
+          cm = fmaxf(cm, xor_lane_c(cm, 32));
+          const float mn = cm > m[nt] + kSlack ? ceilf(cm) : m[nt];
+          const float w = exp2f(m[nt] - mn);
+          m[nt] = mn;
+          l[nt] *= w;
+#pragma unroll
+          for (int d = 0; d < DT; ++d) acc[nt][d] *= w;
+          exponents(sc[nt], fa, fb, kLift - m[nt], z[nt], top);
         }
+      }
+      f16x8 pf[NT][NP];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        if constexpr (F32) {
+          probability_parts(z[nt], l[nt], pf[nt][0], pf[nt][NP - 1]);
+        } else {
+          uint32_t u[4];
+          probabilities(z[nt], l[nt], u);
+          probabilities(z[nt] + 4, l[nt], u + 2);
+          pf[nt][0] = frag(u[0], u[1], u[2], u[3]);
+        }
+      }
+      if constexpr (apart.value) {
+        add_apart<NT, NP, DT>(acc, pf, rva, rvb, [&](int d) { return frag8(pg[0].vd(d), pg[1].vd(d)); });
+      } else {
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
           const f16x8 vf = frag8(pg[0].vd(d), pg[1].vd(d), rva, rvb);
@@ -259,22 +253,46 @@ __global__ void __launch_bounds__(256 * CT, NT == 1 || !F32 ? 2 : 1) k_kv8_attn(
 #pragma unroll
             for (int p = 0; p < NP; ++p) acc[nt][d] = mfma(vf, pf[nt][p], acc[nt][d]);
         }
-      };
+      }
+    };
+    int i0 = 0;
+    for (; i0 < mine; i0 += 32) {
+      const int todo = min(32, mine - i0);
+      if (i0 > 0) {
+        id = pages_at(i0);
+#pragma unroll
+        for (int i = 0; i + 1 < DEPTH; ++i) request(buf[i], i);
+      }
+      enter();
+      if (unit.apart) break;
       // (a ring without copies: a copy would wait for its load)
       for (int i = 0; i < todo; i += DEPTH) {
 #pragma unroll
         for (int u = 0; u < DEPTH; ++u)
           if (i + u < todo) {
             request(buf[(u + DEPTH - 1) % DEPTH], i + u + DEPTH - 1);
-            step(buf[u], i + u);
+            step(buf[u], i0, i + u, std::false_type{});
           }
+      }
+    }
+    // (a loop of its own: with both sums in one, 64 chains of 8 rows over 2300 positions take 102 us, 76 so)
+#pragma unroll 1
+    for (; i0 < mine; i0 += 32) {
+      id = pages_at(i0);
+      enter();
+      const int todo = min(32, mine - i0);
+#pragma unroll 1
+      for (int i = 0; i < todo; ++i) {
+        Page<HD> one[2];
+        request(one, i);
+        step(one, i0, i, std::true_type{});
       }
     }
     if (missing && a.err) atomicOr(a.err, 1u << 2);
 
     // ---- merge the wavefronts --------------------------------------------------------
     const bool direct = x.ns == 1 && a.out != nullptr;   // one split: no join
-    const float back = eref * kDownBy;
+    const float back = unit.at * kDownBy;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       l[nt] += xor_lane_c(l[nt], 16);

@@ -291,6 +291,65 @@ OSP_DEV float query_parts(const float* p, f16x8* hi, f16x8* lo) {
   return kv8_pow2(-up);
 }
 
+// The unit of a wavefront's outputs.  Value codes go into the product relative to the largest value scale
+// so far, as f16: exact down to 2^-15 of it (a code is a multiple of 2^-9, an f16 of 2^-24).  But scales of
+// one pass may span 2^220, and the largest may belong to positions that a row does not see.  A wavefront
+// that meets a scale below 2^-15 of its unit (a page of zeros has one), or whose unit has grown by more
+// than 2^60 (up to there fp32 outputs hold what they had), goes on in a fixed unit, 2^kDown: codes
+// unscaled, a product for each page, which joins the outputs at the page's scale (add_apart).
+struct ValueUnit {
+  float at = 0.f;       // the unit (0: no page yet)
+  float first = 0.f;    // what it was at first
+  bool apart = false;   // it is fixed
+};
+// A chunk's pages with value scales sv (0: none) join.  rel: the factor of a page's codes, or (apart) of
+// its product.  Returns the factor for the outputs so far.
+OSP_DEV float enter_scales(ValueUnit& u, float sv, float& rel) {
+  rel = sv * kDownBy;
+  if (u.apart) return 1.f;
+  const float was = u.at, top = fmaxf(was, wave_max(sv));
+  if (was == 0.f) u.first = top;
+  const float r = top > 0.f ? sv / top : 0.f;
+  u.at = top;
+  u.apart = __builtin_amdgcn_ballot_w64((sv > 0.f && r < 0x1p-15f) || top * 0x1p-60f > u.first) != 0;
+  if (u.apart) {
+    u.at = 1.f / kDownBy;
+    return was > 0.f ? was * kDownBy : 1.f;
+  }
+  rel = r;
+  return was > 0.f ? was / top : 1.f;
+}
+// A lane's share of P for a pair's first (second) page alone.
+OSP_DEV f16x8 page_of_pair(f16x8 p, int second) {
+  const uint4 v = __builtin_bit_cast(uint4, p);
+  return second ? frag(0u, 0u, v.z, v.w) : frag(v.x, v.y, 0u, 0u);
+}
+// acc[] += V P of a pair, a page at a time at its own factor; codes(d): its unscaled codes, dims 16 d ..
+template <int NT, int NP, int DT, typename Codes>
+OSP_DEV void add_apart(f32x4 (&acc)[NT][DT], const f16x8 (&p)[NT][NP], float fa, float fb, Codes codes) {
+#pragma unroll 1
+  for (int k = 0; k < 2; ++k) {
+    const float f = k ? fb : fa;
+    f16x8 one[NT][NP];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int i = 0; i < NP; ++i) one[nt][i] = page_of_pair(p[nt][i], k);
+#pragma unroll
+    for (int d = 0; d < DT; ++d) {
+      const f16x8 vf = codes(d);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        f32x4 t = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < NP; ++i) t = mfma(vf, one[nt][i], t);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[nt][d][e] = __builtin_fmaf(t[e], f, acc[nt][d][e]);
+      }
+    }
+  }
+}
+
 // P = 2^z of a lane's eight exponents as f16 parts hi + lo; its sum joins l.
 OSP_DEV void probability_parts(const float* z, float& l, f16x8& hi, f16x8& lo) {
 #pragma unroll

@@ -94,7 +94,8 @@ __global__ void __launch_bounds__(64 * NW, HD == 64 ? 3 : 2) k_kv8_prompt(Kv8Att
     const int my_pair = wave % PAIRS;
     const long off = is_v ? (long)(a.pool.nkv + g) * (kKv8Page * HD) + qr * 4 * HD + n16 * (HD / 4)
                           : (long)g * (kKv8Page * HD) + n16 * HD + qr * (HD / 4);
-    float eref = 0.f, rel = 0.f;   // largest value scale so far; the chunk's relative to it
+    ValueUnit unit;
+    float rel = 0.f;   // of the chunk's pages
     uint4 raw[RAW];
 
     // pages p_lo / 16 + 64 c + lane of chunk c: id (-1: none), scales
@@ -127,7 +128,7 @@ __global__ void __launch_bounds__(64 * NW, HD == 64 ? 3 : 2) k_kv8_prompt(Kv8Att
       if (is_v) {
         const int t0 = p_lo + (s * PAIRS + my_pair) * 32, at = (s * PAIRS + my_pair) * 2 & 63;
         const bool ok[2] = {lane_i(ids, at) >= 0, lane_i(ids, at + 1) >= 0};
-        const float ra = lane_f(rel, at), rb = lane_f(rel, at + 1);
+        const float ra = unit.apart ? 1.f : lane_f(rel, at), rb = unit.apart ? 1.f : lane_f(rel, at + 1);
         if (t0 + 32 > p_hi || !ok[0] || !ok[1]) {
           // codes past the split, or of a missing page, may be anything: 0 * NaN
 #pragma unroll
@@ -156,21 +157,16 @@ __global__ void __launch_bounds__(64 * NW, HD == 64 ? 3 : 2) k_kv8_prompt(Kv8Att
       }
     };
 
-    // A new chunk's pages: values go into LDS relative to the largest scale so far.
+    // A new chunk's pages: values go into LDS relative to the largest scale so far (ValueUnit).
     auto enter = [&]() {
       missing |= id == -1;
-      const float top = fmaxf(eref, wave_max(fabsf(sv)));
-      if (top > eref) {
-        if (eref > 0.f) {
-          const float f = eref / top;
+      const float f = enter_scales(unit, sv, rel);   // (the same in every wavefront)
+      if (f != 1.f) {
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int d = 0; d < DT; ++d) acc[nt][d] *= f;
-        }
-        eref = top;
+          for (int d = 0; d < DT; ++d) acc[nt][d] *= f;
       }
-      rel = eref > 0.f ? sv / eref : 0.f;
       scales_of(id_next, sk_next, sv_next);
     };
     enter();
@@ -181,7 +177,7 @@ __global__ void __launch_bounds__(64 * NW, HD == 64 ? 3 : 2) k_kv8_prompt(Kv8Att
       stage(0, 0, id);
     }
     __syncthreads();
-    for (int s = 0; s < n_steps; ++s) {
+    auto step = [&](int s, auto apart) {
       const int buf = s & 1, in_chunk = s * PAIRS * 2 & 63;
       if (in_chunk == 0) {
         sk_now = sk;
@@ -261,6 +257,10 @@ __global__ void __launch_bounds__(64 * NW, HD == 64 ? 3 : 2) k_kv8_prompt(Kv8Att
             pf[nt][0] = frag(u[0], u[1], u[2], u[3]);
           }
         }
+        if constexpr (apart.value) {
+          add_apart<NT, NP, DT>(acc, pf, lane_f(rel, at), lane_f(rel, at + 1), [&](int d) { return __builtin_bit_cast(f16x8, vp[d * 64]); });
+          continue;
+        }
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < DT; i += 4) {
@@ -287,7 +287,11 @@ __global__ void __launch_bounds__(64 * NW, HD == 64 ? 3 : 2) k_kv8_prompt(Kv8Att
         stage(s + 1, buf ^ 1, id);
       }
       __syncthreads();
-    }
+    };
+    // (two loops: with both sums in one, a prompt takes a tenth longer)
+    int s0 = 0;
+    for (; s0 < n_steps && !unit.apart; ++s0) step(s0, std::false_type{});
+    for (; s0 < n_steps; ++s0) step(s0, std::true_type{});
     if (missing && a.err) atomicOr(a.err, 1u << 2);
 
     // ---- outputs: lane holds dims 16 d + 4 qr .. + 4 of vector n16 of each tile --------
@@ -301,7 +305,7 @@ __global__ void __launch_bounds__(64 * NW, HD == 64 ? 3 : 2) k_kv8_prompt(Kv8Att
       const int row = x.s.beg + c / group, h = g * group + c % group;
       if (qr == 0 && x.split == 0 && a.row_ns) a.row_ns[(long)row * a.nq + h] = x.ns;
       if (direct) {
-        const float inv = l[nt] > 0.f || l[nt] != l[nt] ? eref / l[nt] : 0.f;
+        const float inv = l[nt] > 0.f || l[nt] != l[nt] ? unit.at / l[nt] : 0.f;
         const long at = (long)row * a.ldo + (long)h * HD + 4 * qr;
         if constexpr (F32) {
           float* o = reinterpret_cast<float*>(a.out) + at;
@@ -328,7 +332,7 @@ __global__ void __launch_bounds__(64 * NW, HD == 64 ? 3 : 2) k_kv8_prompt(Kv8Att
                                                              f32x2_to_bf16x2(acc[nt][d][2] * inv, acc[nt][d][3] * inv));
       } else {
         float* pp = a.part + (((long)row * a.nq + h) * a.n_split + x.split) * (HD + 2);
-        const float back = eref * kDownBy;
+        const float back = unit.at * kDownBy;
         if (qr == 0) {
           pp[0] = a.natural ? (m[nt] > kNoMax ? (m[nt] - kLift + kDown) * kLn2 : -INFINITY) : m[nt];
           pp[1] = l[nt] * kDownBy;
