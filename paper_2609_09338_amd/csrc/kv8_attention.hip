@@ -22,7 +22,8 @@
 //     own rounding.  fp32 rows take P as hi + lo as well.  Maxima, sums and outputs are fp32.
 //   * The running maximum only moves when a score passes it by 2^8 (one ballot a pair, no
 //     cross-lane traffic otherwise), and then to a whole number: outputs are rescaled by powers of
-//     two, exactly.  Sums stay per lane until the end.
+//     two, exactly.  Scores may have any size that fp32 holds (exponents_masked).  Sums stay per lane
+//     until the end.
 // Measured, with the join: one token over 131002 positions (8 kv heads of 128) 56 us, 4.8 TB/s; the
 // next token of 64 requests of 512 to 4095 positions 68 us, 4.2 TB/s (a copy reaches 4.7); 8 chains of 8
 // rows over 4000 positions 25.5 us, 2.6 TB/s; one token over 2048 positions 7 + 3 us of latency.  What
@@ -121,6 +122,7 @@ __global__ void __launch_bounds__(256 * CT, NT == 1 || !F32 ? 2 : 1) k_kv8_attn(
     int lim[NT];
     int lim_lo = 0x7fffffff, lim_hi = 0;
     bool missing = false;   // a visible position has no page
+    bool far = false;       // some vector's maximum is (kFar)
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const int c = c0 + v0 + 16 * nt + n16;
@@ -175,7 +177,7 @@ __global__ void __launch_bounds__(256 * CT, NT == 1 || !F32 ? 2 : 1) k_kv8_attn(
       const float ska = lane_f(sk, 2 * i), skb = lane_f(sk, 2 * i + 1);
       const float rva = lane_f(rel, 2 * i), rvb = lane_f(rel, 2 * i + 1);
       const bool oka = lane_i(ok, 2 * i) != 0, okb = lane_i(ok, 2 * i + 1) != 0;
-      const bool whole = t0 + 32 <= min(lim_lo, s_hi) && oka && okb;
+      const bool whole = t0 + 32 <= min(lim_lo, s_hi) && oka && okb && !far;
       f32x4 sc[NT][2];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) sc[nt][0] = sc[nt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -195,7 +197,7 @@ __global__ void __launch_bounds__(256 * CT, NT == 1 || !F32 ? 2 : 1) k_kv8_attn(
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
         exponents(sc[nt], score_factor(ska, colc[nt]), score_factor(skb, colc[nt]), kLift - m[nt], z[nt], top);
-      // One branch for all that is rare: pairs that some vector sees in part, maxima that move.
+      // One branch for all that is rare: pairs that some vector sees in part, maxima that move or are far.
       if (!whole || __builtin_amdgcn_ballot_w64(top > kLift + kSlack)) {
         if (!whole) {
           // value codes past the context may be anything: 0 * NaN
@@ -221,13 +223,12 @@ __global__ void __launch_bounds__(256 * CT, NT == 1 || !F32 ? 2 : 1) k_kv8_attn(
           float cm = fmaxf(max4(sc[nt][0]) * fa, max4(sc[nt][1]) * fb);
           cm = fmaxf(cm, xor_lane_c(cm, 16));
           cm = fmaxf(cm, xor_lane_c(cm, 32));
-          const float mn = cm > m[nt] + kSlack ? ceilf(cm) : m[nt];
-          const float w = exp2f(m[nt] - mn);
-          m[nt] = mn;
+          const float w = move_max(m[nt], cm);
+          far |= any_far(m[nt]);
           l[nt] *= w;
 #pragma unroll
           for (int d = 0; d < DT; ++d) acc[nt][d] *= w;
-          exponents(sc[nt], fa, fb, kLift - m[nt], z[nt], top);
+          exponents_masked(sc[nt], fa, fb, m[nt], far, z[nt], top);
         }
       }
       f16x8 pf[NT][NP];
@@ -317,7 +318,7 @@ __global__ void __launch_bounds__(256 * CT, NT == 1 || !F32 ? 2 : 1) k_kv8_attn(
       float L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
-        const float f = exp2f(sm_m[w][j] - M);
+        const float f = M > kNoMax ? exp2f(sm_m[w][j] - M) : 0.f;
         L += sm_l[w][j] * f;
         const float4 v = *reinterpret_cast<const float4*>(&sm_o[w][j][e]);
         o[0] += v.x * f;
@@ -377,7 +378,8 @@ __global__ void __launch_bounds__(256) k_kv8_join(Kv8AttnArgs a) {
         for (int e = 0; e < E; ++e) v[k][e] = pp[s * (HD + 2) + 2 + lane * E + e];
       }
       if (s0 == 0) {
-        f = exp2f(m - wave_max(m));
+        const float M = wave_max(m);
+        f = M > kNoMax ? exp2f(m - M) : 0.f;
         L = wave_sum(ls * f);
       }
 #pragma unroll

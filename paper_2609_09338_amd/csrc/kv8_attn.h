@@ -14,9 +14,10 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr float kNoMax = -1.0e30f;   // below any score: a row that has seen nothing
+constexpr float kNoMax = -INFINITY;  // the maximum of a row that has seen nothing
 constexpr float kLift = 6.f;         // P's largest value is 2^kLift, 2^(kLift + kSlack) before the maximum moves
 constexpr float kSlack = 8.f;
+constexpr float kFar = 16777216.f;   // 2^24: from here on neighbouring floats are 2 and more apart
 // Sums and outputs leave a wavefront at 2^-kDown: P's lift and a long context's sum of it take them past
 // fp32 with values from 2^96 on, and nothing that counts falls below (a row's sum is 2^5 at least).
 constexpr float kDown = 24.f, kDownBy = 1.f / (1 << 24);
@@ -377,6 +378,31 @@ OSP_DEV void exponents(const f32x4* s, float fa, float fb, float up, float* z, f
   for (int e = 0; e < 8; ++e) {
     z[e] = __builtin_fmaf(s[e >> 2][e & 3], e < 4 ? fa : fb, up);
     top = fmaxf(top, z[e]);
+  }
+}
+
+// A maximum m takes in the largest of a pair's scores; returns the factor of sums and outputs so far.  (By
+// differences: they are exact where they matter, m + kSlack is not.  Nothing seen yet, -inf: any score moves
+// it, and none leaves it, by NaN.)
+OSP_DEV float move_max(float& m, float cm) {
+  const float was = m;
+  if (cm - m > kSlack) m = ceilf(cm);
+  return m > was ? exp2f(was - m) : 1.f;
+}
+OSP_DEV bool is_far(float m) { return fabsf(m) >= kFar && fabsf(m) < INFINITY; }
+OSP_DEV bool any_far(float m) { return __builtin_amdgcn_ballot_w64(is_far(m)) != 0; }
+// The exponents of a pair that may be masked, or (far) where some vector's maximum lies kFar or more from
+// zero.  There a score's product must be rounded as its maximum's was: what the fma keeps below that rounding
+// is as large as P's whole range, and the largest P would be 0 or infinite.
+OSP_DEV void exponents_masked(const f32x4* s, float fa, float fb, float m, bool far, float* z, float& top) {
+  const float at = m > kNoMax ? m : 0.f;   // (nothing seen: every score is -inf)
+  exponents(s, fa, fb, kLift - at, z, top);
+  if (!far) return;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+#pragma clang fp contract(off)
+    const float t = s[e >> 2][e & 3] * (e < 4 ? fa : fb);
+    z[e] = is_far(m) ? (t - at) + kLift : z[e];
   }
 }
 

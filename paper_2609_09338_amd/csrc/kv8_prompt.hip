@@ -53,7 +53,7 @@ __global__ void __launch_bounds__(64 * NW, HD == 64 ? 3 : 2) k_kv8_prompt(Kv8Att
     float colc[NT], m[NT], l[NT];
     int lim[NT];
     int lim_lo = 0x7fffffff, lim_hi = 0;
-    bool missing = false;
+    bool missing = false, far = false;   // far: some vector's maximum is (kFar)
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const int c = c0 + 16 * nt + n16;
@@ -190,7 +190,7 @@ __global__ void __launch_bounds__(64 * NW, HD == 64 ? 3 : 2) k_kv8_prompt(Kv8Att
         if (t0 >= lim_hi) continue;   // (none of this wavefront's vectors sees the pair, or it has none)
         const bool oka = lane_i(id_now, at) >= 0, okb = lane_i(id_now, at + 1) >= 0;
         const float ska = lane_f(sk_now, at), skb = lane_f(sk_now, at + 1);
-        const bool whole = t0 + 32 <= min(lim_lo, p_hi) && oka && okb;
+        const bool whole = t0 + 32 <= min(lim_lo, p_hi) && oka && okb && !far;
         // A operands are read four ahead of the products that take them (left to itself the compiler
         // reads one, waits for it and uses it).
         f32x4 sc[NT][2];
@@ -223,7 +223,7 @@ __global__ void __launch_bounds__(64 * NW, HD == 64 ? 3 : 2) k_kv8_prompt(Kv8Att
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
           exponents(sc[nt], score_factor(ska, colc[nt]), score_factor(skb, colc[nt]), kLift - m[nt], z[nt], top);
-        // One branch for all that is rare: pairs that some vector sees in part, maxima that move.
+        // One branch for all that is rare: pairs that some vector sees in part, maxima that move or are far.
         if (!whole || __builtin_amdgcn_ballot_w64(top > kLift + kSlack)) {
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
@@ -236,13 +236,12 @@ __global__ void __launch_bounds__(64 * NW, HD == 64 ? 3 : 2) k_kv8_prompt(Kv8Att
             float cm = fmaxf(max4(sc[nt][0]) * fa, max4(sc[nt][1]) * fb);
             cm = fmaxf(cm, xor_lane_c(cm, 16));
             cm = fmaxf(cm, xor_lane_c(cm, 32));
-            const float mn = cm > m[nt] + kSlack ? ceilf(cm) : m[nt];
-            const float w = exp2f(m[nt] - mn);
-            m[nt] = mn;
+            const float w = move_max(m[nt], cm);
+            far |= any_far(m[nt]);
             l[nt] *= w;
 #pragma unroll
             for (int d = 0; d < DT; ++d) acc[nt][d] *= w;
-            exponents(sc[nt], fa, fb, kLift - m[nt], z[nt], top);
+            exponents_masked(sc[nt], fa, fb, m[nt], far, z[nt], top);
           }
         }
         f16x8 pf[NT][NP];
