@@ -716,8 +716,9 @@ bool run_body(osprey_handle* h, RowMeta rows, const int32_t* cu, int B, const fl
     // (one launch fewer per layer); otherwise the merge kernel writes o.
     const bool merge_in_o = gemv_attn_supported(c.dtype, rows.max_rows, nq * hd, hd, sp.n_split);
     if (h->kv8) {
-      run_rows_qkv(h, a, W.o);
-      a.q_prep = W.o;
+      // (not in W.o: the merge writes it, and a timed attention reads its queries again)
+      run_rows_qkv(h, a, W.split);
+      a.q_prep = W.split;
     }
     run_attention(h, a, !merge_in_o);
     // O projection + residual
