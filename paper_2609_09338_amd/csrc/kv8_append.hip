@@ -326,6 +326,15 @@ OSP_DEV int rope_row(const Kv8AppendArgs& a, int row) {
 template <int C> OSP_DEV float dpp(float v) { return dpp_f<C>(v); }
 template <int C> OSP_DEV double dpp(double v) { return dpp_d<C>(v); }
 
+// The sum over a head's LPH lanes.
+template <int LPH, typename S> OSP_DEV S head_sum(S v) {
+  v += dpp<kDppXor1>(v);
+  v += dpp<kDppXor2>(v);
+  if constexpr (LPH >= 8) v += dpp<kDppHalfMirror>(v);
+  if constexpr (LPH >= 16) v += dpp<kDppMirror>(v);
+  return v;
+}
+
 // Queries of RQ rows from row0 on: HD / (2 V) lanes a head, V values of either half a lane; every
 // row's values are requested before the first is used.
 template <typename T, int HD, int RQ>
@@ -358,13 +367,26 @@ OSP_DEV void do_queries(const Kv8AppendArgs& a, int row0, int rows, int h0, int 
       acc_t ss = 0;
 #pragma unroll
       for (int i = 0; i < 2 * V; ++i) ss += x[i] * x[i];
-      ss += dpp<kDppXor1>(ss);
-      ss += dpp<kDppXor2>(ss);
-      if constexpr (LPH >= 8) ss += dpp<kDppHalfMirror>(ss);
-      if constexpr (LPH >= 16) ss += dpp<kDppMirror>(ss);
+      ss = head_sum<LPH>(ss);
       acc_t inv;
-      if constexpr (sizeof(T) == 4) inv = 1.0 / sqrt(ss / HD + (double)a.eps);
-      else inv = 1.0f / sqrtf(ss / HD + a.eps);
+      if constexpr (sizeof(T) == 4) {
+        inv = 1.0 / sqrt(ss / HD + (double)a.eps);
+      } else {
+        float eps = a.eps;
+        // (not so for NaN) squares near the ends of fp32: the same of the head times a power of two
+        if (!(ss < 0x1p120f && ss / HD + eps > 0x1p-90f)) {
+          const float by = ss < 1.f ? 0x1p60f : 0x1p-70f;
+          eps = eps * by * by;
+          ss = 0.f;
+#pragma unroll
+          for (int i = 0; i < 2 * V; ++i) {
+            x[i] *= by;
+            ss += x[i] * x[i];
+          }
+          ss = head_sum<LPH>(ss);
+        }
+        inv = 1.0f / sqrtf(ss / HD + eps);
+      }
 #pragma unroll
       for (int i = 0; i < 2 * V; ++i) x[i] *= inv * (acc_t)gain(a.q_norm, a.g_bf16, (i / V) * (HD / 2) + j * V + i % V);
     }
