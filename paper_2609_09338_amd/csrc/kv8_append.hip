@@ -19,6 +19,7 @@
 #include <type_traits>
 
 #include "kv8.h"
+#include "kv8_rows.h"
 
 namespace osp {
 namespace {
@@ -335,10 +336,10 @@ template <int LPH, typename S> OSP_DEV S head_sum(S v) {
   return v;
 }
 
-// Queries of RQ rows from row0 on: HD / (2 V) lanes a head, V values of either half a lane; every
+// Queries of RQ rows of q from row0 on: HD / (2 V) lanes a head, V values of either half a lane; every
 // row's values are requested before the first is used.
 template <typename T, int HD, int RQ>
-OSP_DEV void do_queries(const Kv8AppendArgs& a, int row0, int rows, int h0, int lane) {
+OSP_DEV void do_queries(const Kv8AppendArgs& a, int row0, QueryRows q, int h0, int lane) {
   constexpr int V = Vec<T>::N, LPH = HD / (2 * V);
   const int h = h0 + lane / LPH, j = lane % LPH;
   if (h >= a.nq) return;   // (whole groups of lanes that reduce together)
@@ -346,19 +347,17 @@ OSP_DEV void do_queries(const Kv8AppendArgs& a, int row0, int rows, int h0, int 
   int pos[RQ];
 #pragma unroll
   for (int r = 0; r < RQ; ++r) {
-    const int row = min(row0 + r, rows - 1);
+    const int row = row_read(q, row0 + r);
 #pragma unroll
     for (int k = 0; k < 2; ++k)
       load_n<T, V>(a.q, (long)row * a.ldq + (long)h * HD + k * (HD / 2) + j * V, a.ks, a.split, xs[r] + k * V);
   }
 #pragma unroll
-  for (int r = 0; r < RQ; ++r) pos[r] = rope_row(a, min(row0 + r, rows - 1));
-  const int first = a.r.cu ? a.r.cu[0] : 0;
+  for (int r = 0; r < RQ; ++r) pos[r] = rope_row(a, row_read(q, row0 + r));
 #pragma unroll
   for (int r = 0; r < RQ; ++r) {
     const int row = row0 + r;
-    if (row >= rows) return;
-    if (row < first) continue;
+    if (!has_row(q, row)) continue;
     typedef typename std::conditional<sizeof(T) == 4, double, float>::type acc_t;
     acc_t x[2 * V];
 #pragma unroll
@@ -419,10 +418,12 @@ OSP_DEV void do_queries(const Kv8AppendArgs& a, int row0, int rows, int h0, int 
     }
   }
 }
-// The rows that queries are formed for: those of the sequences.
-OSP_DEV int query_rows(const Kv8AppendArgs& a) {
+// Queries of group i of RQ rows, heads from h0 on.
+template <typename T, int HD, int RQ>
+OSP_DEV void query_group(const Kv8AppendArgs& a, int i, int h0, int lane) {
   const int total = a.r.count ? min(*a.r.count, a.r.rows) : a.r.rows;
-  return a.r.cu ? min(total, a.r.cu[a.r.B]) : total;
+  const QueryRows q = query_rows(total, a.r.cu ? a.r.cu[0] : 0, a.r.cu ? a.r.cu[a.r.B] : total);
+  if (group_has_rows(q, i, RQ)) do_queries<T, HD, RQ>(a, i * RQ, q, h0, lane);
 }
 
 // One new token a sequence: a wavefront owns the token's key and value of one kv head, a rotation
@@ -434,8 +435,7 @@ __global__ void __launch_bounds__(256) k_kv8_append_one(Kv8AppendArgs a, int uni
   const int lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
   if (w >= units) {
-    const int rows = query_rows(a), row = (w - units) / q_per_row;
-    if (row < rows) do_queries<T, HD, 1>(a, row, rows, ((w - units) % q_per_row) * (64 / (HD / (2 * Vec<T>::N))), lane);
+    query_group<T, HD, 1>(a, (w - units) / q_per_row, ((w - units) % q_per_row) * (64 / (HD / (2 * Vec<T>::N))), lane);
     return;
   }
   const int g = w % a.pool.nkv, b = w / a.pool.nkv;
@@ -550,12 +550,9 @@ __global__ void __launch_bounds__(256) k_kv8_append(Kv8AppendArgs a, int units, 
     else append_values<T, HD>(a, r0, off, hi - lo, g, blk, sc, lane);
     return;
   }
-  const int v = w - units, h0 = (v % q_per_row) * (64 / (HD / (2 * Vec<T>::N))), rows = query_rows(a);
-  if (many) {
-    if (v / q_per_row * kQueryRows < rows) do_queries<T, HD, kQueryRows>(a, v / q_per_row * kQueryRows, rows, h0, lane);
-  } else if (v / q_per_row < rows) {
-    do_queries<T, HD, 1>(a, v / q_per_row, rows, h0, lane);
-  }
+  const int v = w - units, h0 = (v % q_per_row) * (64 / (HD / (2 * Vec<T>::N)));
+  if (many) query_group<T, HD, kQueryRows>(a, v / q_per_row, h0, lane);
+  else query_group<T, HD, 1>(a, v / q_per_row, h0, lane);
 }
 
 // One block per (sequence, kv head, keys or values): the positions base .. base + n - 1 take the
