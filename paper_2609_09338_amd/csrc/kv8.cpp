@@ -184,7 +184,8 @@ OSPREY_API int osprey_kv8_append(const osprey_kv8_cache* c, const osprey_kv8_app
   k.ldo = a->q_out_stride;
   k.q_scale = 1.f;
   k.err = a->err;
-  launch_kv8_append(k, (hipStream_t)hip_stream);
+  if (!launch_kv8_append(k, (hipStream_t)hip_stream))
+    return fail(OSPREY_E_UNSUPPORTED, "%d rows of %d kv heads and %d query heads: more than a grid holds", a->rows, c->n_kv_heads, k.nq);
   return done();
 }
 

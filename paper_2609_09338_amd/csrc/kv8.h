@@ -74,7 +74,8 @@ struct Kv8AppendArgs {
   float q_scale;
   uint32_t* err;            // (nullable)
 };
-void launch_kv8_append(const Kv8AppendArgs& a, hipStream_t st);
+// False, and nothing enqueued: more blocks and rows than a grid holds.
+bool launch_kv8_append(const Kv8AppendArgs& a, hipStream_t st);
 
 struct Kv8KeepArgs {
   Kv8Pool pool;

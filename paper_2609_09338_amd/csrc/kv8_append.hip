@@ -671,33 +671,28 @@ __global__ void __launch_bounds__(256) k_kv8_keep(Kv8KeepArgs a) {
 
 }  // namespace
 
+// (a grid holds fewer than 2^32 threads)
+constexpr long kMaxWaves = (1L << 26) - 4;
 template <typename T, int HD>
-void launch_append(const Kv8AppendArgs& a, hipStream_t st) {
+bool launch_append(const Kv8AppendArgs& a, hipStream_t st) {
   constexpr int hpw = 64 / (HD / (2 * Vec<T>::N));   // heads a wavefront
   const int q_per_row = a.q ? (a.nq + hpw - 1) / hpw : 1;
-  const bool one = !a.r.cu && (a.r.B > 1 || a.r.rows == 1);
-  if (one) {
-    const int units = a.r.B * a.pool.nkv;
-    const long waves = units + (a.q ? (long)a.r.rows * q_per_row : 0);
-    hipLaunchKernelGGL((k_kv8_append_one<T, HD>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, st, a, units, q_per_row);
-    return;
-  }
-  const int units = (a.r.rows / 16 + 2 * a.r.B) * a.pool.nkv * 2;
   const long q_waves = a.q ? (long)a.r.rows * q_per_row : 0;
+  const bool one = !a.r.cu && (a.r.B > 1 || a.r.rows == 1);
+  const long units = one ? (long)a.r.B * a.pool.nkv : (a.r.rows / 16 + 2L * a.r.B) * a.pool.nkv * 2;
   // Four rows a wavefront where that still fills the chip (256 CUs of 16 such wavefronts).
-  const int many = q_waves >= kManyQueries;
+  const int many = !one && q_waves >= kManyQueries;
   const long waves = units + (many ? (long)((a.r.rows + kQueryRows - 1) / kQueryRows) * q_per_row : q_waves);
-  hipLaunchKernelGGL((k_kv8_append<T, HD>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, st, a, units, q_per_row, many);
+  if (waves > kMaxWaves) return false;
+  const dim3 grid((unsigned)((waves + 3) / 4));
+  if (one) hipLaunchKernelGGL((k_kv8_append_one<T, HD>), grid, dim3(256), 0, st, a, (int)units, q_per_row);
+  else hipLaunchKernelGGL((k_kv8_append<T, HD>), grid, dim3(256), 0, st, a, (int)units, q_per_row, many);
+  return true;
 }
 
-void launch_kv8_append(const Kv8AppendArgs& a, hipStream_t st) {
-  if (a.x_bf16) {
-    if (a.hd == 128) launch_append<bf16_t, 128>(a, st);
-    else launch_append<bf16_t, 64>(a, st);
-  } else {
-    if (a.hd == 128) launch_append<float, 128>(a, st);
-    else launch_append<float, 64>(a, st);
-  }
+bool launch_kv8_append(const Kv8AppendArgs& a, hipStream_t st) {
+  if (a.x_bf16) return a.hd == 128 ? launch_append<bf16_t, 128>(a, st) : launch_append<bf16_t, 64>(a, st);
+  return a.hd == 128 ? launch_append<float, 128>(a, st) : launch_append<float, 64>(a, st);
 }
 
 void launch_kv8_keep(const Kv8KeepArgs& a, hipStream_t st) {

@@ -370,7 +370,7 @@ int hip_last() {
   hipError_t e = hipGetLastError();
   if (g_refused) {
     g_refused = false;
-    return fail(OSPREY_E_UNSUPPORTED, "a streaming product takes at most %d rows (%d prepared)", kLmMaxRows, kSkMaxRows);
+    return fail(OSPREY_E_UNSUPPORTED, "a kernel does not take the rows of a pass (a streaming product at most %d, %d prepared)", kLmMaxRows, kSkMaxRows);
   }
   if (e != hipSuccess) return fail(OSPREY_E_DEVICE, "kernel launch: %s", hipGetErrorString(e));
   return ok();
@@ -512,7 +512,7 @@ void run_rows_qkv(osprey_handle* h, const AttnArgs& a, float* q_out) {
   k.q_bf16 = kv8_many(a);
   k.q_scale = a.scale;
   k.err = a.err;
-  launch_kv8_append(k, h->stream);
+  if (!launch_kv8_append(k, h->stream)) g_refused = true;
 }
 
 // The attention of an 8-bit handle's pass, into the same partials as the others'.
@@ -1407,7 +1407,7 @@ OSPREY_API int osprey_kv_append(osprey_handle* h, int32_t slot, int32_t n, const
       q.pool = kv8_pool(h, l, slot, nullptr);
       q.k = (const uint16_t*)k + l * layer;
       q.v = (const uint16_t*)v + l * layer;
-      launch_kv8_append(q, h->stream);
+      if (!launch_kv8_append(q, h->stream)) return fail(OSPREY_E_UNSUPPORTED, "%d positions: more than a grid holds", n);
     }
   }
   launch_kv_append(h->cfg.dtype, h->kv, k, v, h->kv8 ? 0 : h->cfg.n_layers, n, h->cfg.n_kv_heads, h->cfg.head_dim,
