@@ -260,8 +260,9 @@ OSP_DEV void mask_scores(f32x4& s, uint32_t sight, int qr) {
   for (int e = 0; e < 4; ++e)
     if (!(v >> e & 1)) s[e] = -INFINITY;
 }
-// The factor of a page's scores: never zero, so that a masked one stays -inf.
-OSP_DEV float score_factor(float sk, float colc) { return fmaxf(sk * colc, 1.2e-38f); }
+// The factor of a page's scores: never zero, so that a masked one stays -inf (a large query over small keys
+// has a use for the smallest).
+OSP_DEV float score_factor(float sk, float colc) { return fmaxf(sk * colc, 1.4e-45f); }
 OSP_DEV float max4(f32x4 s) { return fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])); }
 
 // The power of two that takes a query vector's largest magnitude into [2^13, 2^14).

@@ -152,3 +152,25 @@ def test_rows_that_see_nothing_are_zeros_beside_rows_of_far_scores():
             for i in range(rows):
                 want = ref.read(0, i)[1][0] if masks[i] else torch.zeros(hd, dtype=torch.float64)
                 assert torch.equal(out[i].cpu().double(), want.expand(group, hd)), (group, dtype, i)
+
+
+@pytest.mark.parametrize("rows", [1, 40])
+def test_large_queries_over_the_smallest_scales_keep_their_small_scores(rows):
+    """Products of 2^125 with codes, a block's scale of 2^-100 and a small softmax scale: the factor of the
+    scores lies below fp32's normal numbers (7 bits of it are left at 2^-142, all that a score of 2^-17 needs)."""
+    hd, n = 64, 64
+    cache = make_cache(1, n // 16, 1, hd, 3)
+    k = torch.zeros((n, 1, hd), device=DEV)
+    k[:, 0, 3] = torch.where(torch.arange(n, device=DEV) % 2 == 0, 256.0, -256.0) * 2.0 ** -100
+    v = torch.where(torch.arange(n, device=DEV) % 2 == 0, 1.0, -1.0)[:, None, None].expand(n, 1, hd).contiguous()
+    bd().kv8_append(cache, k, v, ints([0]), cu_rows=ints([0, n]))
+    q = torch.zeros((rows, 2, hd), device=DEV, dtype=BF)
+    q[:, :, 3] = 2.0 ** 117
+    for scale, z in ((2.0 ** -24, 2.0), (2.0 ** -28, 2.0 ** -3), (2.0 ** -42, 2.0 ** -17)):
+        out = attend(cache, n - rows, rows, q, 1, scale=scale)
+        even = torch.arange(n - rows, n) // 2 + 1.0
+        odd = (torch.arange(n - rows, n) + 1) // 2
+        up, down = even * torch.exp(torch.tensor(z, dtype=torch.float64)), odd * torch.exp(torch.tensor(-z, dtype=torch.float64))
+        want = ((up - down) / (up + down))[:, None, None]
+        # the factor's rounding of 2^-8 of the score, P's 2^-11, the sums' 2^-18, the output's 2^-8
+        assert bool(((out - want).abs() <= 2.0 ** -8 * want.abs() + 2 * z * 2.0 ** -8 + 2.0 ** -11 + 2.0 ** -18).all()), (scale, z)
