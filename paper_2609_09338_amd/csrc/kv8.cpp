@@ -222,7 +222,8 @@ OSPREY_API int osprey_kv8_attention(const osprey_kv8_cache* c, const osprey_kv8_
     return fail(OSPREY_E_INVALID, "max_rows %d and max_context %d must be at least 1", a->max_rows, a->max_context);
   if (a->tree_mask && a->max_rows > 128) return fail(OSPREY_E_SHAPE, "a tree mask takes at most 128 rows a sequence, max_rows is %d", a->max_rows);
   if ((uintptr_t)a->tree_mask & 7) return fail(OSPREY_E_INVALID, "tree_mask must be 8-byte aligned");
-  if (!(a->scale > 0.f && std::isfinite(a->scale))) return fail(OSPREY_E_INVALID, "scale must be > 0");
+  // (scores are taken to base 2)
+  if (!(a->scale > 0.f && std::isfinite(a->scale * 1.4426950408889634f))) return fail(OSPREY_E_INVALID, "scale must be > 0 and finite over ln 2");
   if ((rc = check_buffer("q", a->q, a->q_stride, a->n_q_heads, c->head_dim, a->dtype))) return rc;
   if ((rc = check_buffer("out", a->out, a->out_stride, a->n_q_heads, c->head_dim, a->dtype))) return rc;
   const int n_cu = compute_units();
