@@ -153,7 +153,6 @@ __global__ void __launch_bounds__(256 * CT, NT == 1 || !F32 ? 2 : 1) k_kv8_attn(
 
     ValueUnit unit;
     float sk = 0.f, rel = 0.f;   // scales of the chunk's pages (keys; values: enter_scales)
-    int ok = 0;
     auto enter = [&]() {
       float sv = 0.f;
       sk = 0.f;
@@ -163,7 +162,6 @@ __global__ void __launch_bounds__(256 * CT, NT == 1 || !F32 ? 2 : 1) k_kv8_attn(
         sv = s[1];
       }
       missing |= id == -1;
-      ok = id >= 0;
       const float f = enter_scales(unit, sv, rel);
       if (f != 1.f) {
 #pragma unroll
@@ -176,7 +174,7 @@ __global__ void __launch_bounds__(256 * CT, NT == 1 || !F32 ? 2 : 1) k_kv8_attn(
       const int t0 = pair_at(i0 + i);
       const float ska = lane_f(sk, 2 * i), skb = lane_f(sk, 2 * i + 1);
       const float rva = lane_f(rel, 2 * i), rvb = lane_f(rel, 2 * i + 1);
-      const bool oka = lane_i(ok, 2 * i) != 0, okb = lane_i(ok, 2 * i + 1) != 0;
+      const bool oka = lane_i(id, 2 * i) >= 0, okb = lane_i(id, 2 * i + 1) >= 0;
       const bool whole = t0 + 32 <= min(lim_lo, s_hi) && oka && okb && !far;
       f32x4 sc[NT][2];
 #pragma unroll
@@ -276,7 +274,7 @@ __global__ void __launch_bounds__(256 * CT, NT == 1 || !F32 ? 2 : 1) k_kv8_attn(
           }
       }
     }
-    // (a loop of its own: with both sums in one, 64 chains of 8 rows over 2300 positions take 102 us, 76 so)
+    // (a loop of its own: with both sums in one, 64 chains of 8 rows over 2300 positions take 102 us, 74 so)
 #pragma unroll 1
     for (; i0 < mine; i0 += 32) {
       id = pages_at(i0);
