@@ -77,7 +77,9 @@ typedef enum {
 /* OSPREY_BF16_KV8 (configurations only): bf16 weights, gains and taps, and a KV cache held
  * in 8 bits as osprey_kv8_cache describes it: half of a bf16 cache's bytes.  Keys and values
  * are rounded to 4 significant bits; the queries of passes of more than 32 query vectors per
- * kv head and sequence to bf16.  Every call works as with OSPREY_BF16. */
+ * kv head and sequence to bf16.  Every call works as with OSPREY_BF16, but a slot's page keeps
+ * what dropped positions (rejected drafts, truncations) did to its scale and older codes:
+ * osprey_kv8_append_args. */
 typedef enum { OSPREY_F32 = 0, OSPREY_BF16 = 1, OSPREY_BF16_KV8 = 2 } osprey_dtype;
 
 /* Drafter and pool shape.  Weights, norm gains, taps and the KV cache share
@@ -458,7 +460,12 @@ typedef struct {
  * the smallest power of two, at least 2^-100, that takes the new elements to at most 448; a
  * block that holds older positions (the first new one is not the page's first) keeps at least
  * its old scale, and where the scale grows the older codes are rounded to it.  Codes are
- * rounded to nearest, ties to even, keys from double. */
+ * rounded to nearest, ties to even, keys from double.
+ * That is for good: rows that are dropped again (rejected drafts) leave the older positions of
+ * their first page, and those that take their places there, as coarse as the largest element
+ * among them made the block.  Who must not have that copies the page (codes and scales) before
+ * drafts are appended and puts it back before the accepted rows are appended again.
+ * Positions behind the last new one in its page lose what they held. */
 typedef struct {
   int32_t rows;
   const int32_t* cu_rows;     /* [batch + 1] or NULL */
@@ -485,11 +492,15 @@ typedef struct {
  * positions that row r sees, the new rows' own positions already appended.  Row j of sequence
  * b sees the positions up to and including cached[b] + j; with a tree mask the positions
  * before cached[b], and cached[b] + i where bit i % 64 of tree_mask[2 r + i / 64] is set (at
- * most 128 rows a sequence).  A row that sees nothing gets zeros.  Sums are held in fp32.
+ * most 128 rows a sequence).  A row that sees nothing gets zeros.  Sums are held in fp32, and
+ * so are scores (times log2 e) and a bf16 query's products with codes (magnitudes up to 448):
+ * those that pass fp32 give no numbers, or count as not seen.  Values of any size are taken,
+ * also where blocks of one pass lie 2^220 apart.
  * Query head h reads kv head h n_kv_heads / n_q_heads.
  * max_rows (at least the largest row count of a sequence) and max_context (the longest context
  * with its new rows that the call is planned for) only choose the kernel and how the work is
- * split: longer sequences are still attended right.  The work is dealt out on the device from
+ * split: longer sequences are still attended right (and short ones in a call planned for long
+ * ones, up to a quarter slower).  The work is dealt out on the device from
  * the lengths there, so that a captured call serves every later length.
  * The workspace holds the splits' partial outputs and nothing that outlives a call: calls in
  * order on one stream may share one, calls that can overlap may not. */
@@ -504,7 +515,7 @@ typedef struct {
   int32_t n_q_heads;          /* a multiple of n_kv_heads */
   const void* q;              /* row r at q + r * q_stride (elements): [n_q_heads][head_dim] */
   int64_t q_stride;
-  float scale;                /* > 0 (usually 1 / sqrt(head_dim)) */
+  float scale;                /* > 0, at most 2.3e38 (usually 1 / sqrt(head_dim)) */
   void* out;                  /* row r at out + r * out_stride */
   int64_t out_stride;
   void* workspace;            /* 16-byte aligned */
@@ -514,7 +525,8 @@ typedef struct {
 
 /* Arguments of osprey_kv8_keep: position base[b] + i takes the keys and values of position
  * base[b] + path[b][i], i < n[b], by the append's rule for scales (a row of osprey_verify_tree's
- * accept_path with base = the position of node 0, and n = accept_len).  A path ascends. */
+ * accept_path with base = the position of node 0, and n = accept_len).  A path ascends.
+ * Positions behind the last kept one in its page lose what they held. */
 typedef struct {
   const int32_t* base;        /* [batch] */
   const int32_t* path;        /* [batch][path_stride] */
@@ -525,6 +537,8 @@ typedef struct {
 
 /* The calls are enqueued on hip_stream (NULL: the null stream) of the current device, which
  * must be the buffers'; they allocate nothing, keep nothing, and can be captured into a graph.
+ * An append of more blocks and rows than a grid holds is refused (over about 2^29 rows x kv
+ * heads).
  * osprey_kv8_workspace_bytes: the workspace of an attention call with these sizes (0: invalid,
  * or no device). */
 int osprey_kv8_append(const osprey_kv8_cache* c, const osprey_kv8_append_args* a, void* hip_stream);

@@ -5,8 +5,9 @@
 // one of 16 hd value codes, e4m3 (OCP; finite, magnitudes up to 448), each with one scale, a
 // power of two: value = code * scale.  With scales that are powers of two a code moves from
 // one scale to a larger one by its exponent alone: exact until it falls below 2^-6 of the
-// scale, where e4m3 steps are even anyway, so a block whose scale has to grow while tokens
-// are appended loses nothing that one quantised in a single pass would have kept.
+// scale, where e4m3 steps are even.  There a block whose scale grew while tokens were appended
+// has been rounded twice, and a code may be a step from what a single pass would have kept (the
+// first rounding can land on a tie).  A scale never shrinks while older tokens stay.
 //
 // Layout of a block.  Keys are token-major [16][hd]: lane (token l % 16, quarter l / 16) of a
 // wavefront reads hd / 4 contiguous bytes, its share of every K step of S^T = K Q^T.  Values

@@ -15,7 +15,8 @@
 // rate here), and rounded once: codes are those of the definition, not of a summation order.  fp32
 // queries are formed so too (6.3e-8 of their size off in fp32, a rounding's 2.5e-8 so; 6000 rows of
 // 32 heads 60 and 62 us); bf16 queries, whose rounding is 2^-8, in fp32 (8000 rows of 32 heads of 64
-// 31 us, in double 38), and values need no more.
+// 31 us, in double 38; 33 since rows outside the sequences are not read), times a power of two where
+// their squares would not be fp32; and values need no more.
 #include <type_traits>
 
 #include "kv8.h"

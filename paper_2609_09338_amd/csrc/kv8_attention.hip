@@ -24,9 +24,9 @@
 //     cross-lane traffic otherwise), and then to a whole number: outputs are rescaled by powers of
 //     two, exactly.  Scores may have any size that fp32 holds (exponents_masked).  Sums stay per lane
 //     until the end.
-// Measured, with the join: one token over 131002 positions (8 kv heads of 128) 56 us, 4.8 TB/s; the
-// next token of 64 requests of 512 to 4095 positions 68 us, 4.2 TB/s (a copy reaches 4.7); 8 chains of 8
-// rows over 4000 positions 25.5 us, 2.6 TB/s; one token over 2048 positions 7 + 3 us of latency.  What
+// Measured, with the join: one token over 131002 positions (8 kv heads of 128) 57 us, 4.7 TB/s; the
+// next token of 64 requests of 512 to 4095 positions 68 us, 4.2 TB/s (a copy reaches 4.8); 8 chains of 8
+// rows over 4000 positions 23.3 us, 2.8 TB/s; one token over 2048 positions 7 + 3 us of latency.  What
 // runs once a wavefront costs its instruction fetches: the code before and after the loop is kept
 // short (converting the queries there and unrolled merges took 16 rows over 136 positions 26 us, 13 so).
 #include <algorithm>
@@ -433,10 +433,11 @@ void launch_form(const Kv8AttnArgs& a, int form, dim3 grid, hipStream_t st) {
 // wavefront each over the same pages (8 wavefronts a block: less code and no registers spilled, but
 // every page converted twice and half as many pages in flight) or both in one wavefront.  Which, goes by
 // the (kv head, position) pairs of the pass.  8 rows of 4 heads, us, each / both, with 128-wide heads:
-// 8 sequences of 2000 positions and 8 kv heads 18 / 24, 8 of 3950 26 / 28, 10 of 3950 32 / 32, 12 of 3950
-// 39 / 34, 64 of 2300 124 / 74, 32 of 3950 and 2 kv heads 27 / 29, 64 so 47 / 39; 64-wide: 8 of 3950 and
-// 8 kv heads 15.6 / 15.7, 32 of 3950 34 / 32.  fp32, where both in one leave one wavefront a SIMD: 8 of
-// 3950 27 / 36, 16 of 3950 47 / 46, 64 of 2300 128 / 82.  More vectors: kv8_prompt.hip.
+// 8 sequences of 2000 positions and 8 kv heads 19 / 25, 8 of 3950 24 / 28, 10 of 3950 29 / 33, 12 of 3950
+// 37 / 37, 64 of 2300 124 / 74, 32 of 3950 and 2 kv heads 25 / 29, 64 so 41 / 44; 64-wide: 8 of 3950 and
+// 8 kv heads 16.4 / 16.9, 32 of 3950 34 / 36.  fp32, where both in one leave one wavefront a SIMD: 8 of
+// 3950 27 / 37, 16 of 3950 43 / 51, 64 of 2300 127 / 82.  (The bound dates from slower kernels of the
+// first kind; up to twice the pairs the two differ by 4 us at most.)  More vectors: kv8_prompt.hip.
 int kv8_attention_form(int x_bf16, int group, int max_rows, long positions, int nkv) {
   const long c = (long)group * max_rows;
   if (c <= 16) return kKv8Narrow;

@@ -18,11 +18,11 @@
 //   * The softmax is kept to what a vector ALU must do a score: one fma, half a maximum, an exp2, half
 //     a conversion and half a dot product with ones (the sum, of the rounded P).  All that is rare
 //     (masks, maxima that move) sits behind one branch a pair of pages.
-// 4 x 1000 rows over 6000 to 9000 positions, 32 heads of 128 over 8: 551 us, 970 TFLOP/s (a large
-// bf16 matrix product reaches 1250 here); a prompt of 4099 rows 167 us, 825 TFLOP/s.  The same with
+// 4 x 1000 rows over 6000 to 9000 positions, 32 heads of 128 over 8: 565 us, 948 TFLOP/s (a large
+// bf16 matrix product reaches 1250 here); a prompt of 4099 rows 168 us, 820 TFLOP/s.  The same with
 // one wavefront a token range and no LDS (kv8_attention.hip at 64 vectors) took 1010 and 373 us.
-// fp32 rows take two products each (hi + lo), so 16 vectors a wavefront: a prompt of 4000 rows 256 us
-// (128-wide heads), 155 us (64-wide).
+// fp32 rows take two products each (hi + lo), so 16 vectors a wavefront: a prompt of 4000 rows 267 us
+// (128-wide heads), 163 us (64-wide).
 #include <algorithm>
 #include <type_traits>
 
