@@ -18,9 +18,10 @@ constexpr float kNoMax = -INFINITY;  // the maximum of a row that has seen nothi
 constexpr float kLift = 6.f;         // P's largest value is 2^kLift, 2^(kLift + kSlack) before the maximum moves
 constexpr float kSlack = 8.f;
 constexpr float kFar = 16777216.f;   // 2^24: from here on neighbouring floats are 2 and more apart
-// Sums and outputs leave a wavefront at 2^-kDown: P's lift and a long context's sum of it take them past
-// fp32 with values from 2^96 on, and nothing that counts falls below (a row's sum is 2^5 at least).
-constexpr float kDown = 24.f, kDownBy = 1.f / (1 << 24);
+// Sums and outputs leave a wavefront at 2^-kDown: P reaches 2^14, and a sum of 2^18 such of the largest
+// values fits.  Nothing that counts falls below: a row's sum is 2^5 at least, and the largest value of a
+// block of the smallest scale, 2^-91, is 2^31 of the smallest floats there.
+constexpr float kDown = 32.f, kDownBy = 0x1p-32f;
 
 OSP_DEV uint32_t h2(f16x2 v) { return __builtin_bit_cast(uint32_t, v); }
 // Two of a dword's codes as f16, times a power of two.

@@ -137,3 +137,23 @@ def test_small_values_before_large_ones_in_a_later_chunk(rows, dtype):
     sees[:, 8000:8960] = False
     want, tol = S.attention(ref_of(cache), 0, q, sees, hd ** -0.5, dtype)
     assert bool(((out.cpu().double() - want).abs() <= tol).all())
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("spread", [False, True])
+@pytest.mark.parametrize("rows", [1, 8, 40])
+def test_many_of_the_largest_values_in_one_sum(rows, spread, dtype):
+    """6000 values of 3e38 whose probabilities lie 2^7 above what the first pages' maximum makes 2^6: sums of
+    2^25 times the largest float, in one split, over blocks of one scale and beside a page of zeros."""
+    nkv, hd, n = 1, 64, 6000
+    cache = make_cache(1, n // 16 + 1, nkv, hd, 3)
+    k = torch.zeros((n, nkv, hd), device=DEV)
+    k[128:, :, 0] = 1.0
+    v = 3.0e38 * (1 - 0.2 * torch.rand((n, nkv, hd), generator=gen_of(15), device=DEV))
+    if spread:
+        v[3200:3216] = 0.0
+    bd().kv8_append(cache, k, v, ints([0]), cu_rows=ints([0, n]))
+    q = torch.zeros((rows, 4, hd), device=DEV)
+    q[:, :, 0] = 5.1875 * hd ** 0.5
+    check(cache, [n - rows], [rows], q.to(dtype), max_context=1)
+    check(cache, [n - rows], [rows], q.to(dtype), max_context=n)
